@@ -1,6 +1,7 @@
 /*
  * aq.h -- C ABI of the additively-quantized (AQ) layer forward for AMD
- * Instinct MI355X (gfx950).
+ * Instinct MI355X (gfx950), with 4-bit layers and the losses that a low-bit
+ * model is tuned with (further down).
  *
  * Operation (AQUATIC-Diff, arXiv 2506.05960, Sec. 2.4 eq. (4) and Sec. 3.1.1):
  * the weight matrix W [C_out][K] of a linear or im2col-lowered convolution
@@ -344,6 +345,152 @@ aq_status aq_layer_choose_path(const aq_layer* layer, int64_t tokens, aq_path* o
 
 /* Release the layer's device memory (synchronises the device).  NULL is a no-op. */
 aq_status aq_layer_destroy(aq_layer* layer);
+
+/* ---- linear layers of 4-bit codes with group scales ---- */
+
+/*
+ * Uniform scalar quantization (AQUATIC-Diff Sec. 2.3 eq. (3)), the format of
+ * layers whose weights are not additively quantized.  Row i of the weight
+ * matrix [out_features][in_features] is split into groups of `group`
+ * consecutive inputs (the last may be shorter), each with one scale and one
+ * zero point:
+ *
+ *     W[i][k] = s[i][j] * (q[i][k] - z[i][j]),   j = k / group,   q, z in 0..15
+ */
+typedef struct aq_usq aq_usq; /* opaque, owned by the library */
+
+typedef struct {
+    int32_t out_features;  /* >= 1                                                             */
+    int32_t in_features;   /* a multiple of 8                                                  */
+    int32_t group;         /* inputs a scale covers: 32, 64 or a multiple of 128               */
+    int32_t dtype;         /* aq_dtype of X, dY, dX and the scales: F16 | BF16                 */
+    int32_t y_dtype;       /* aq_dtype of Y: F32 | F16 | BF16                                  */
+    int64_t max_tokens;    /* every call needs n <= max_tokens                                 */
+} aq_usq_desc;
+
+/*
+ * Create a 4-bit layer on the current HIP device: validate, copy and lay out
+ * the weights in library-owned device memory.  Synchronous; the caller may
+ * free its buffers on return.
+ *   codes   host, [out_features][in_features / 2], two codes a byte: input 2 b
+ *           in the lower half of byte b, input 2 b + 1 in the upper half
+ *   scales  host, [out_features][ceil(in_features / group)] in desc->dtype
+ *           (bf16 as raw bits)
+ *   zeros   host, the scales' shape, uint8, each at most 15 (scanned:
+ *           AQ_ERR_INVALID_ARGUMENT); NULL: every zero point is 8
+ *   out     receives the handle (set to NULL on failure)
+ * Formats outside the descriptor's comments that are valid otherwise return
+ * AQ_ERR_UNSUPPORTED.  Without a GPU: AQ_ERR_DEVICE.
+ */
+aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* scales, const uint8_t* zeros,
+                        aq_usq** out);
+
+/*
+ * Forward Y = X * W^T on `stream`; asynchronous, allocates nothing and never
+ * synchronises.  Weights are not rounded: the integers q - z are multiplied
+ * with the inputs exactly, sums are fp32, and each group's sum is scaled.
+ * Summation orders are fixed for each n: repeated calls give identical bits.
+ *   X   device [n][in_features] in desc->dtype; 16-byte aligned
+ *   Y   device [n][out_features] in desc->y_dtype; 16-byte aligned
+ *   n   1 <= n <= max_tokens
+ * The layer's device has to be the current one (AQ_ERR_INVALID_ARGUMENT).
+ */
+aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void* stream);
+
+/*
+ * Input gradient dX = dY * W on `stream`: the gradient that passes through a
+ * frozen 4-bit layer.  W is rounded once to desc->dtype, sums are fp32.
+ *   dY  device [n][out_features] in desc->dtype; 16-byte aligned
+ *   dX  device [n][in_features] in desc->dtype, overwritten; 16-byte aligned
+ * The first call on a layer allocates its workspace (synchronous, not under
+ * graph capture): the decoded weights of a slab of inputs, at most 32 MiB (or
+ * of 128 inputs), and, unless out_features is a multiple of 8, a copy of dY
+ * for max_tokens tokens.  Later calls are asynchronous and allocate nothing.
+ * Gradients of one layer share that workspace: serialise them on one stream.
+ * Errors and determinism as for aq_usq_forward.
+ */
+aq_status aq_usq_input_grad(aq_usq* layer, const void* dY, void* dX, int64_t n, void* stream);
+
+/* Release the layer's device memory (synchronises the device).  NULL is a no-op. */
+aq_status aq_usq_destroy(aq_usq* layer);
+
+/* ---- losses over a vocabulary ---- */
+
+/* What a low-bit model is tuned with (Sec. 3.2): the losses and their
+ * gradients, in the layouts aq_layer_codebook_grad and aq_usq_input_grad take. */
+typedef struct aq_loss aq_loss; /* opaque, owned by the library */
+
+typedef struct {
+    int32_t vocab;         /* tokens of the vocabulary, >= 1                                   */
+    int32_t features;      /* the head's inputs, a multiple of 8; 0: no cross entropy          */
+    int32_t dtype;         /* aq_dtype of logits or of X and W, and of every gradient but dloss:
+                              F16 | BF16, or F32 without features                              */
+    int64_t max_tokens;    /* every call needs n <= max_tokens                                 */
+} aq_loss_desc;
+
+/* Create the losses of one vocabulary on the current HIP device, with the row
+ * statistics of the cross entropy: 8 bytes per token and 256 vocabulary rows. */
+aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
+
+/*
+ * Softmax cross entropy of the logits z = X * W^T and its gradients, on
+ * `stream`, without keeping the logits: their maxima and sums are formed
+ * tile by tile, and the gradient forms them again for one piece of the
+ * vocabulary after the other.
+ *     loss[t] = log(sum_v exp(z[t][v])) - z[t][targets[t]]
+ *     dz[t][v] = dloss[t] * (softmax(z[t])[v] - (v == targets[t]))
+ *     dX = dz * W,   dW = dz^T * X
+ *   X        device [n][features] in desc->dtype; 16-byte aligned
+ *   W        device [vocab][features] in desc->dtype; 16-byte aligned
+ *   targets  device [n] int64.  A negative target does not count: its loss and
+ *            its row of dz are zero, whatever its row of X holds.  A target
+ *            past the vocabulary makes its loss NaN, and the gradients with it
+ *   dloss    device [n] fp32, the gradient of the objective with respect to
+ *            each loss, finite; NULL: ones
+ *   loss     device [n] fp32, overwritten
+ *   dX       device [n][features] in desc->dtype, overwritten; 16-byte
+ *            aligned; NULL: not computed
+ *   dW       device [vocab][features] in desc->dtype, overwritten; 16-byte
+ *            aligned; NULL: not computed
+ *   n        1 <= n <= max_tokens
+ * Sums are fp32; dz is rounded once to desc->dtype before the products (scaled
+ * so that the largest |dloss| lies just below 2^15).
+ * The first call with dX or dW allocates their workspace (synchronous, not
+ * under graph capture): per token and per feature 2 bytes for each vocabulary
+ * row of a piece (at most 128 MiB each, or 256 rows), and copies of X.  Later
+ * calls are asynchronous and allocate nothing.  Calls on one handle share its
+ * workspace: serialise them on one stream.  Summation orders are fixed:
+ * repeated calls give identical bits.
+ */
+aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void* W, const int64_t* targets,
+                                const float* dloss, float* loss, void* dX, void* dW, int64_t n, void* stream);
+
+/*
+ * Distillation from a teacher's top logits, on `stream`: with p the teacher's
+ * softmax over the tokens that its list holds and q the student's over the
+ * whole vocabulary, both at the temperature T,
+ *     loss[t] = T^2 * sum_j p[t][j] * (log p[t][j] - log q[t][ids[t][j]])
+ *     dlogits[t][v] = dloss[t] * T * (q[t][v] - sum of p[t][j] with ids[t][j] == v)
+ *   logits   device [n][vocab] in desc->dtype; 16-byte aligned
+ *   ids      device [n][top] int32, the listed tokens.  A negative entry is
+ *            empty, and so is one whose teacher logit is -infinity; a row
+ *            without any other has loss 0 and gradient 0.  A token may be
+ *            listed twice.  An id past the vocabulary makes its row NaN
+ *   teacher  device [n][top] in desc->dtype, the teacher's logits
+ *   top      1 <= top <= 1024
+ *   dloss    device [n] fp32; NULL: ones
+ *   loss     device [n] fp32, overwritten
+ *   dlogits  device [n][vocab] in desc->dtype, overwritten; 16-byte aligned;
+ *            may be `logits` itself; NULL: not computed
+ *   n        1 <= n <= max_tokens
+ * Asynchronous, allocates nothing; sums are fp32 in a fixed order.
+ */
+aq_status aq_loss_distill(aq_loss* loss_handle, const void* logits, const int32_t* ids, const void* teacher,
+                          int32_t top, float temperature, const float* dloss, float* loss, void* dlogits, int64_t n,
+                          void* stream);
+
+/* Release the handle's device memory (synchronises the device).  NULL is a no-op. */
+aq_status aq_loss_destroy(aq_loss* loss_handle);
 
 /* Message for the last failing call on this thread ("" if none). */
 const char* aq_last_error(void);

@@ -1,4 +1,5 @@
-"""MI355X-native additively-quantized (AQ) layer: forward and codebook gradient.
+"""MI355X-native additively-quantized (AQ) layer: forward and codebook gradient;
+4-bit layers with group scales; distillation and cross-entropy losses.
 
 The product is ``libaq.so`` (HIP kernels for gfx950 behind the C ABI in
 ``include/aq.h``); this package holds its sources (``csrc/``), the build
@@ -27,5 +28,17 @@ from .aq import (  # noqa: F401
     OPTION_CODES,
     aq_layer_choose_path,
     aq_layer_destroy,
+    USQLayer,
+    VocabLoss,
+    aq_usq_desc,
+    aq_usq_create,
+    aq_usq_forward,
+    aq_usq_input_grad,
+    aq_usq_destroy,
+    aq_loss_desc,
+    aq_loss_create,
+    aq_loss_cross_entropy,
+    aq_loss_distill,
+    aq_loss_destroy,
     aq_version,
 )

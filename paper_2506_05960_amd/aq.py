@@ -34,6 +34,8 @@ EXPORTED = ("aq_layer_create", "aq_layer_forward", "aq_layer_forward_static", "a
             "aq_layer_codebook_grad",
             "aq_layer_set_path", "aq_layer_set_option", "aq_layer_get_option", "aq_layer_set_launch_events",
             "aq_layer_last_launches", "aq_layer_describe", "aq_layer_choose_path", "aq_layer_destroy",
+            "aq_usq_create", "aq_usq_forward", "aq_usq_input_grad", "aq_usq_destroy",
+            "aq_loss_create", "aq_loss_cross_entropy", "aq_loss_distill", "aq_loss_destroy",
             "aq_last_error", "aq_version")
 
 
@@ -60,6 +62,15 @@ class aq_layer_desc(ctypes.Structure):
         ("in_w", ctypes.c_int32),
         ("max_tokens", ctypes.c_int64),
     ]
+
+
+class aq_usq_desc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("out_features", "in_features", "group", "dtype", "y_dtype")] + [
+        ("max_tokens", ctypes.c_int64)]
+
+
+class aq_loss_desc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("vocab", "features", "dtype")] + [("max_tokens", ctypes.c_int64)]
 
 
 _lib = None
@@ -90,11 +101,21 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.aq_layer_describe.argtypes = [vp, i64, ctypes.c_char_p, i64]
     lib.aq_layer_choose_path.argtypes = [vp, i64, ctypes.POINTER(ctypes.c_int)]
     lib.aq_layer_destroy.argtypes = [vp]
+    lib.aq_usq_create.argtypes = [ctypes.POINTER(aq_usq_desc), vp, vp, vp, ctypes.POINTER(vp)]
+    lib.aq_usq_forward.argtypes = [vp, vp, vp, i64, vp]
+    lib.aq_usq_input_grad.argtypes = [vp, vp, vp, i64, vp]
+    lib.aq_usq_destroy.argtypes = [vp]
+    lib.aq_loss_create.argtypes = [ctypes.POINTER(aq_loss_desc), ctypes.POINTER(vp)]
+    lib.aq_loss_cross_entropy.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.aq_loss_distill.argtypes = [vp, vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, i64, vp]
+    lib.aq_loss_destroy.argtypes = [vp]
     for f in ("aq_layer_create", "aq_layer_forward", "aq_layer_forward_static", "aq_layer_prepare",
               "aq_layers_prepare", "aq_layer_decode",
               "aq_layer_codebook_grad",
               "aq_layer_set_path", "aq_layer_set_option", "aq_layer_get_option", "aq_layer_set_launch_events",
-              "aq_layer_last_launches", "aq_layer_describe", "aq_layer_choose_path", "aq_layer_destroy"):
+              "aq_layer_last_launches", "aq_layer_describe", "aq_layer_choose_path", "aq_layer_destroy",
+              "aq_usq_create", "aq_usq_forward", "aq_usq_input_grad", "aq_usq_destroy",
+              "aq_loss_create", "aq_loss_cross_entropy", "aq_loss_distill", "aq_loss_destroy"):
         getattr(lib, f).restype = ctypes.c_int
     lib.aq_last_error.restype = ctypes.c_char_p
     lib.aq_last_error.argtypes = []
@@ -215,6 +236,46 @@ def aq_layer_choose_path(handle: int, tokens: int) -> str:
 
 def aq_layer_destroy(handle: Optional[int]) -> None:
     _check(load_library().aq_layer_destroy(handle))
+
+
+def aq_usq_create(desc: aq_usq_desc, codes: int, scales: int, zeros: Optional[int]) -> int:
+    """``codes``, ``scales`` and ``zeros`` are host addresses; None for ``zeros``: every zero point is 8."""
+    h = ctypes.c_void_p()
+    _check(load_library().aq_usq_create(ctypes.byref(desc), codes, scales, zeros, ctypes.byref(h)))
+    return h.value
+
+
+def aq_usq_forward(handle: int, X: int, Y: int, n: int, stream: int) -> None:
+    _check(load_library().aq_usq_forward(handle, X, Y, n, stream))
+
+
+def aq_usq_input_grad(handle: int, dY: int, dX: int, n: int, stream: int) -> None:
+    _check(load_library().aq_usq_input_grad(handle, dY, dX, n, stream))
+
+
+def aq_usq_destroy(handle: Optional[int]) -> None:
+    _check(load_library().aq_usq_destroy(handle))
+
+
+def aq_loss_create(desc: aq_loss_desc) -> int:
+    h = ctypes.c_void_p()
+    _check(load_library().aq_loss_create(ctypes.byref(desc), ctypes.byref(h)))
+    return h.value
+
+
+def aq_loss_cross_entropy(handle: int, X: int, W: int, targets: int, dloss: Optional[int], loss: int,
+                          dX: Optional[int], dW: Optional[int], n: int, stream: int) -> None:
+    _check(load_library().aq_loss_cross_entropy(handle, X, W, targets, dloss, loss, dX, dW, n, stream))
+
+
+def aq_loss_distill(handle: int, logits: int, ids: int, teacher: int, top: int, temperature: float,
+                    dloss: Optional[int], loss: int, dlogits: Optional[int], n: int, stream: int) -> None:
+    _check(load_library().aq_loss_distill(handle, logits, ids, teacher, top, temperature, dloss, loss, dlogits, n,
+                                          stream))
+
+
+def aq_loss_destroy(handle: Optional[int]) -> None:
+    _check(load_library().aq_loss_destroy(handle))
 
 
 def aq_version() -> str:
@@ -442,6 +503,186 @@ class AQLayer:
     def close(self) -> None:
         if getattr(self, "handle", None):
             aq_layer_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---- 4-bit layers and losses ----
+
+def _rows(what: str, t) -> int:
+    """Rows of the matrix ``t`` (its other checks come from ``_check_tensor``)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[0] < 1:
+        raise ValueError(f"{what} must be a torch matrix with at least one row")
+    return t.shape[0]
+
+
+def _host_array(what: str, a, dtype, shape):
+    """Contiguous host torch tensor of ``a`` (tensor or numpy array), or ValueError unless ``dtype`` and ``shape`` fit."""
+    import torch
+    if not isinstance(a, torch.Tensor):
+        a = np.asarray(a)
+        if dtype == torch.bfloat16 and a.dtype in (np.uint16, np.int16):   # bf16 as raw bits
+            a = torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).view(torch.bfloat16)
+        else:
+            a = torch.from_numpy(np.ascontiguousarray(a))
+    if a.device.type != "cpu":
+        raise ValueError(f"{what} must be in host memory, got {a.device}")
+    if a.dtype != dtype:
+        raise ValueError(f"{what} must have dtype {dtype}, got {a.dtype}")
+    if a.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(a.shape)}")
+    return a.contiguous()
+
+
+def _output(what: str, out, dtype, shape, device, like):
+    """The tensor ``out``, checked, or a new one where it is True; None where it is None or False."""
+    import torch
+    if out is None or out is False:
+        return None
+    if out is True:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _check_tensor(what, out, (dtype,), shape, device)
+    return out
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class USQLayer:
+    """A device-resident linear layer of 4-bit codes with group scales.
+
+    ``codes`` is a host array [C_out, K / 2] of uint8 with two codes a byte (the
+    lower half first), ``scales`` [C_out, ceil(K / group)] in ``dtype`` ("f16" or
+    "bf16") and ``zeros`` the same shape in uint8 (None: 8 everywhere):
+    W[i, k] = scales[i, k // group] * (code[i, k] - zeros[i, k // group]).
+    Every tensor argument is checked as in ``AQLayer``.
+    """
+
+    def __init__(self, codes, scales, zeros=None, *, group: int = 128, dtype: str = "f16",
+                 y_dtype: Optional[str] = None, max_tokens: int):
+        import torch
+        y_dtype = dtype if y_dtype is None else y_dtype
+        if dtype not in ("f16", "bf16") or y_dtype not in ("f16", "bf16", "f32"):
+            raise ValueError("dtype must be f16 or bf16, y_dtype f16, bf16 or f32")
+        if not isinstance(group, int) or group < 1:
+            raise ValueError("group must be a positive int")
+        shape = tuple(codes.shape)
+        if len(shape) != 2 or min(shape) < 1:
+            raise ValueError(f"codes must be a matrix, got shape {shape}")
+        self.C_out, self.K = shape[0], 2 * shape[1]
+        G = -(-self.K // group)
+        codes = _host_array("codes", codes, torch.uint8, (self.C_out, self.K // 2))
+        scales = _host_array("scales", scales, _torch_dtype(dtype), (self.C_out, G))
+        if zeros is not None:
+            zeros = _host_array("zeros", zeros, torch.uint8, (self.C_out, G))
+        self.group, self.dtype, self.y_dtype, self.max_tokens = group, dtype, y_dtype, max_tokens
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else None
+        desc = aq_usq_desc(self.C_out, self.K, group, DTYPE_CODES[dtype], DTYPE_CODES[y_dtype], max_tokens)
+        self.handle = aq_usq_create(desc, codes.data_ptr(), scales.data_ptr(), _ptr(zeros))
+
+    def forward(self, x, out=None, stream=None):
+        """Y [n, C_out] for the device tensor ``x`` [n, K]; returns ``out``."""
+        n = _rows("x", x)
+        _check_tensor("x", x, (_torch_dtype(self.dtype),), (n, self.K), self.device)
+        out = _output("out", True if out is None else out, _torch_dtype(self.y_dtype), (n, self.C_out), self.device, x)
+        st = stream if stream is not None else _current_stream(x.device.index)
+        aq_usq_forward(self.handle, x.data_ptr(), out.data_ptr(), n, st)
+        return out
+
+    __call__ = forward
+
+    def input_grad(self, dy, out=None, stream=None):
+        """dX [n, K] for the output gradient ``dy`` [n, C_out] (in ``dtype``); returns ``out``."""
+        n = _rows("dy", dy)
+        dt = _torch_dtype(self.dtype)
+        _check_tensor("dy", dy, (dt,), (n, self.C_out), self.device)
+        out = _output("out", True if out is None else out, dt, (n, self.K), self.device, dy)
+        st = stream if stream is not None else _current_stream(dy.device.index)
+        aq_usq_input_grad(self.handle, dy.data_ptr(), out.data_ptr(), n, st)
+        return out
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            aq_usq_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class VocabLoss:
+    """The losses of one vocabulary, with their gradients.
+
+    ``features``: inputs of the head, for ``cross_entropy`` (None: ``distill`` only).
+    ``dtype``: "f16" or "bf16", or "f32" for ``distill`` alone.  Gradient arguments
+    are None (not computed), True (a new tensor) or the tensor to write.
+    """
+
+    def __init__(self, vocab: int, *, features: Optional[int] = None, dtype: str = "bf16", max_tokens: int):
+        import torch
+        if dtype not in ("f16", "bf16", "f32"):
+            raise ValueError("dtype must be f16, bf16 or f32")
+        if features is not None and features < 1:
+            raise ValueError("features must be a positive int or None")
+        self.vocab, self.features, self.dtype, self.max_tokens = vocab, features, dtype, max_tokens
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else None
+        self.handle = aq_loss_create(aq_loss_desc(vocab, features or 0, DTYPE_CODES[dtype], max_tokens))
+
+    def _row_args(self, n, dloss, loss, like):
+        import torch
+        if dloss is not None:
+            _check_tensor("dloss", dloss, (torch.float32,), (n,), self.device)
+        return _output("loss", True if loss is None else loss, torch.float32, (n,), self.device, like)
+
+    def cross_entropy(self, x, w, targets, dloss=None, loss=None, dx=None, dw=None, stream=None):
+        """(loss [n], dX or None, dW or None) of the head ``w`` [vocab, features] on ``x`` [n, features] for the
+        next tokens ``targets`` [n] (int64; negative: not counted), with ``dloss`` [n] (None: ones) the gradient
+        with respect to each loss; see ``aq_loss_cross_entropy``."""
+        import torch
+        if self.features is None:
+            raise ValueError("created without features: distillation only")
+        n, dt = _rows("x", x), _torch_dtype(self.dtype)
+        _check_tensor("x", x, (dt,), (n, self.features), self.device)
+        _check_tensor("w", w, (dt,), (self.vocab, self.features), self.device)
+        _check_tensor("targets", targets, (torch.int64,), (n,), self.device)
+        loss = self._row_args(n, dloss, loss, x)
+        dx = _output("dx", dx, dt, (n, self.features), self.device, x)
+        dw = _output("dw", dw, dt, (self.vocab, self.features), self.device, x)
+        st = stream if stream is not None else _current_stream(x.device.index)
+        aq_loss_cross_entropy(self.handle, x.data_ptr(), w.data_ptr(), targets.data_ptr(), _ptr(dloss),
+                              loss.data_ptr(), _ptr(dx), _ptr(dw), n, st)
+        return loss, dx, dw
+
+    def distill(self, logits, ids, teacher, temperature: float = 1.0, dloss=None, loss=None, grad=None, stream=None):
+        """(loss [n], gradient or None) of the student's ``logits`` [n, vocab] against the teacher's logits
+        ``teacher`` [n, top] of the tokens ``ids`` [n, top] (int32; negative: empty); see ``aq_loss_distill``."""
+        import torch
+        n, dt = _rows("logits", logits), _torch_dtype(self.dtype)
+        _check_tensor("logits", logits, (dt,), (n, self.vocab), self.device)
+        if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or ids.shape[1] < 1:
+            raise ValueError("ids must be a torch matrix with at least one column")
+        _check_tensor("ids", ids, (torch.int32,), (n, ids.shape[1]), self.device)
+        _check_tensor("teacher", teacher, (dt,), tuple(ids.shape), self.device)
+        loss = self._row_args(n, dloss, loss, logits)
+        grad = _output("grad", grad, dt, (n, self.vocab), self.device, logits)
+        st = stream if stream is not None else _current_stream(logits.device.index)
+        aq_loss_distill(self.handle, logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), ids.shape[1],
+                        temperature, _ptr(dloss), loss.data_ptr(), _ptr(grad), n, st)
+        return loss, grad
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            aq_loss_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

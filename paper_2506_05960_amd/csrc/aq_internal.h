@@ -46,6 +46,10 @@ constexpr int kMaxSplitK = 8;   // most workgroups sharing one output tile along
 // name and template arguments, so that the caller's timing events bracket it.
 void note_launch(hipStream_t st, const char* kernel, std::initializer_list<int> template_args);
 
+// Record the message of a failing call (aq_last_error) and return its status.
+aq_status api_fail(aq_status status, const char* message);
+aq_status api_hip_fail(hipError_t e, const char* what);
+
 // Raise a kernel's dynamic-LDS limit to at least `bytes` on the current
 // device (once per kernel and device; thread-safe).
 hipError_t ensure_dynamic_lds(const void* kernel, size_t bytes);

@@ -172,6 +172,17 @@ aq_status hip_fail(hipError_t e, const char* what) {
     return fail(AQ_ERR_DEVICE, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+}  // namespace
+
+namespace aq {
+
+aq_status api_fail(aq_status status, const char* message) { return fail(status, message); }
+aq_status api_hip_fail(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+}  // namespace aq
+
+namespace {
+
 // Starts the launch trace of one entry-point call: event 0 is recorded on the
 // call's stream before its first launch.  A stream under graph capture gets
 // no event records (this runtime has no external event nodes).  A failed

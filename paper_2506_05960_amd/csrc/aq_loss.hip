@@ -1,0 +1,669 @@
+// Losses over a vocabulary and their gradients: distillation from a teacher's
+// top logits, and softmax cross entropy of a head's logits without keeping the
+// logits.  Entry points and kernels.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "aq_gemm.h"
+
+using aq::api_fail;
+using aq::api_hip_fail;
+
+struct aq_loss {
+    aq_loss_desc desc;
+    int device;
+    int piece;             // cross entropy: vocabulary rows a piece of the gradient covers
+    uint8_t* d_zero;       // 256 zero bytes
+    float2* d_part;        // [vocabulary tile][max_tokens] maximum and sum of exponentials
+    float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then {scale, 1 / scale}
+    // gradient workspace, allocated by the first call that needs it
+    uint16_t* d_dl;        // [max_tokens][piece] logits' gradient of a piece
+    uint16_t* d_dlt;       // [piece][tokens] the same, transposed
+    uint16_t* d_wt;        // [features][piece] the piece's head rows, transposed
+    uint16_t* d_xt;        // [features][tokens] inputs, transposed
+    float* d_dx;           // [max_tokens][features] input gradient of the pieces so far
+};
+
+namespace aq {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kMaxTop = 1024;
+
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// (m, s) of two disjoint parts of a row: maximum, and sum of 2^(c (z - m)).
+__device__ __forceinline__ void merge(float& m, float& s, float om, float os, float c) {
+    const float nm = fmaxf(m, om);
+    const float b = nm == -INFINITY ? 0.0f : nm;    // nothing finite yet: both sums are zero
+    s = s * exp2_fast((m - b) * c) + os * exp2_fast((om - b) * c);
+    m = nm;
+}
+
+// ---- distillation ----
+
+template <int DT>
+struct Store {
+    static constexpr int kVec = DT == AQ_F32 ? 4 : 8;   // values of 16 bytes
+};
+
+template <int DT>
+__device__ __forceinline__ void unpack(const u32x4& v, float (&o)[Store<DT>::kVec]) {
+    if constexpr (DT == AQ_F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __uint_as_float(v[e]);
+    } else if constexpr (DT == AQ_BF16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[2 * e] = __uint_as_float(v[e] << 16);
+            o[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[2 * e] = f16_to_f32((uint16_t)v[e]);
+            o[2 * e + 1] = f16_to_f32((uint16_t)(v[e] >> 16));
+        }
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4 pack(const float (&o)[Store<DT>::kVec]) {
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (DT == AQ_F32) v[e] = __float_as_uint(o[e]);
+        else v[e] = (uint32_t)f32_to_tile<DT>(o[2 * e]) | (uint32_t)f32_to_tile<DT>(o[2 * e + 1]) << 16;
+    }
+    return v;
+}
+
+template <int DT>
+__device__ __forceinline__ void store_as(void* p, int64_t i, float v) {
+    if constexpr (DT == AQ_F32) static_cast<float*>(p)[i] = v;
+    else static_cast<uint16_t*>(p)[i] = f32_to_tile<DT>(v);
+}
+
+struct DistillArgs {
+    const void* logits;
+    const int32_t* ids;
+    const void* teacher;
+    const float* dloss;
+    float* loss;
+    void* grad;
+    int64_t n;
+    int V, top;
+    float c;               // log2(e) / temperature
+    float T;
+};
+
+template <int DT, int THREADS>
+__device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t row) {
+    constexpr int VEC = Store<DT>::kVec;
+    constexpr int WAVES = THREADS / 64;
+    __shared__ float s_m[WAVES], s_s[WAVES];
+    __shared__ float s_p[kMaxTop], s_z[kMaxTop];
+    __shared__ int32_t s_id[kMaxTop];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int V = a.V, top = a.top;
+    const int64_t base = row * V;
+    const int head = min(V, (int)((VEC - base % VEC) % VEC));
+    const int nvec = (V - head) / VEC;
+    const int tail0 = head + nvec * VEC;
+    const u32x4* body = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.logits) +
+                                                       (base + head) * (16 / VEC));
+
+    // ---- pass 1: maximum and sum of exponentials; the listed logits ----
+    float m = -INFINITY, s = 0.0f;
+    auto take = [&](float z) {
+        if (z > m) {
+            s *= exp2_fast((m - z) * a.c);
+            m = z;
+        }
+        const float b = m == -INFINITY ? 0.0f : m;
+        s += exp2_fast((z - b) * a.c);
+    };
+    for (int v = tid; v < nvec; v += THREADS) {
+        float z[VEC];
+        unpack<DT>(body[v], z);
+        float vm = z[0];
+#pragma unroll
+        for (int e = 1; e < VEC; ++e) vm = fmaxf(vm, z[e]);
+        if (vm > m) {
+            s *= exp2_fast((m - vm) * a.c);
+            m = vm;
+        }
+        const float b = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += exp2_fast((z[e] - b) * a.c);
+    }
+    if (tid < head) take(load_as_f32<DT>(a.logits, base + tid));
+    if (tid < V - tail0) take(load_as_f32<DT>(a.logits, base + tail0 + tid));
+    bool bad = false;                       // an id past the vocabulary
+    for (int j = tid; j < top; j += THREADS) {
+        int32_t id = a.ids[row * top + j];
+        float t = load_as_f32<DT>(a.teacher, row * top + j);
+        if (id >= V) bad = true;
+        if (id < 0 || id >= V || t == -INFINITY) {
+            id = -1;
+            t = -INFINITY;
+        }
+        s_id[j] = id;
+        s_p[j] = t;
+        s_z[j] = id >= 0 ? load_as_f32<DT>(a.logits, base + id) : 0.0f;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), a.c);
+    if (lane == 0) {
+        s_m[wave] = m;
+        s_s[wave] = s;
+    }
+    bad = __syncthreads_or(bad);
+    m = s_m[0];
+    s = s_s[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) merge(m, s, s_m[w], s_s[w], a.c);
+    // log2 of a token's probability; the maximum leaves first, while the difference is exact or small
+    const float ls = bad ? NAN : __builtin_amdgcn_logf(s);
+    auto log2q = [&](float z) { return __builtin_fmaf(z - m, a.c, -ls); };
+
+    // ---- the teacher's distribution over its list (every wave computes its sums) ----
+    float tm = -INFINITY, ts = 0.0f;
+    bool nan_t = false;
+    for (int j = lane; j < top; j += 64) {
+        tm = fmaxf(tm, s_p[j]);
+        nan_t |= s_p[j] != s_p[j];
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) tm = fmaxf(tm, __shfl_xor(tm, o));
+    const bool counts = tm != -INFINITY || __any(nan_t) || bad;
+    const float tb = tm == -INFINITY ? 0.0f : tm;
+    for (int j = lane; j < top; j += 64) ts += exp2_fast((s_p[j] - tb) * a.c);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) ts += __shfl_xor(ts, o);
+    const float tl = __builtin_amdgcn_logf(ts);
+    __syncthreads();                                  // s_p read by every wave
+    if (wave == 0) {
+        float l = 0.0f;
+        for (int j = lane; j < top; j += 64) {
+            const float lp = (s_p[j] - tb) * a.c - tl;          // log2 p
+            const float p = exp2_fast(lp);
+            if (p > 0.0f || p != p) l += p * (lp - log2q(s_z[j]));
+            s_p[j] = s_id[j] >= 0 ? p : 0.0f;
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
+        if (bad) l = NAN;
+        if (lane == 0) a.loss[row] = counts ? a.T * a.T * kLn2 * l : 0.0f;
+    }
+    if (!a.grad) return;
+
+    // ---- pass 2: the gradient ----
+    const float g = counts ? a.T * (a.dloss ? a.dloss[row] : 1.0f) : 0.0f;
+    u32x4* out = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.grad) + (base + head) * (16 / VEC));
+    auto value = [&](float z) { return counts ? g * exp2_fast(log2q(z)) : 0.0f; };
+    for (int v = tid; v < nvec; v += THREADS) {
+        float z[VEC];
+        unpack<DT>(body[v], z);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) z[e] = value(z[e]);
+        out[v] = pack<DT>(z);
+    }
+    if (tid < head) store_as<DT>(a.grad, base + tid, value(load_as_f32<DT>(a.logits, base + tid)));
+    if (tid < V - tail0)
+        store_as<DT>(a.grad, base + tail0 + tid, value(load_as_f32<DT>(a.logits, base + tail0 + tid)));
+    if (!counts) return;
+    __syncthreads();                                  // probabilities in s_p
+    // the listed tokens: a token's first entry carries the whole mass of its entries; the thread
+    // that wrote the token's value writes it again, so the two stores are in order
+    for (int j = 0; j < top; ++j) {
+        const int32_t id = s_id[j];
+        if (id < 0) continue;
+        int owner;
+        if (id < head) owner = id;
+        else if (id >= tail0) owner = id - tail0;
+        else owner = ((id - head) / VEC) % THREADS;
+        if (owner != tid) continue;
+        float p = 0.0f;
+        bool first = true;
+        for (int i = 0; i < top; ++i)
+            if (s_id[i] == id) {
+                if (i < j) first = false;
+                p += s_p[i];
+            }
+        if (first) store_as<DT>(a.grad, base + id, g * (exp2_fast(log2q(s_z[j])) - p));
+    }
+}
+
+// One workgroup a row (a launch holds fewer than 2^32 threads).
+constexpr int64_t kMaxRowBlocks = 1 << 20;
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS) distill_kernel(DistillArgs a) {
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        distill_row<DT, THREADS>(a, row);
+        __syncthreads();
+    }
+}
+
+// ---- cross entropy ----
+
+struct RowState {          // arrays of n tokens each
+    const int64_t* targets;
+    const float* dloss;
+    float* zt;             // the target's logit
+    float* top;            // the largest logit
+    float* ls;             // log2 of the sum of exponentials above it
+    float* w;              // row weight of the gradient, 0 for a token that does not count
+    float* loss;
+    float* scale;          // {scale, 1 / scale} of the stored logits' gradient
+};
+
+// D rows are vocabulary rows, D columns tokens: a lane's values all belong to
+// one token, so a tile's maximum and sum are reductions over registers.
+template <int WM, int WN, int AM, int AN>
+struct StatsEpilogue {
+    float2* part;          // [tiles_m][n]
+    RowState rs;
+    __device__ void operator()(const floatx16 (&acc)[AM][AN], int tm, int m0, int n0, int M, int N, uint8_t* lds) const {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
+        float2* red = reinterpret_cast<float2*>(lds);            // [WM][BN]
+        constexpr int BN = WN * AN * 32;
+        __syncthreads();                                         // the last chunk is read
+#pragma unroll
+        for (int b = 0; b < AN; ++b) {
+            const int col = wn * AN * 32 + b * 32 + l32;
+            const int t = n0 + col;
+            const int64_t target = t < N ? rs.targets[t] : -1;
+            float m = -INFINITY;
+#pragma unroll
+            for (int a = 0; a < AM; ++a)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int v = m0 + (wm * AM + a) * 32 + gemm_row(r, hi);
+                    if (v < M) m = fmaxf(m, acc[a][b][r]);
+                    if (v < M && v == target) rs.zt[t] = acc[a][b][r];
+                }
+            const float bm = m == -INFINITY ? 0.0f : m;
+            float s = 0.0f;
+#pragma unroll
+            for (int a = 0; a < AM; ++a)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int v = m0 + (wm * AM + a) * 32 + gemm_row(r, hi);
+                    if (v < M) s += exp2_fast((acc[a][b][r] - bm) * kLog2e);
+                }
+            merge(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32), kLog2e);
+            if (hi == 0) red[wm * BN + col] = make_float2(m, s);
+        }
+        __syncthreads();
+        for (int col = tid; col < BN; col += GemmTile<WM, WN, AM, AN>::kThreads) {
+            if (n0 + col >= N) continue;
+            float2 v = red[col];
+#pragma unroll
+            for (int w = 1; w < WM; ++w) merge(v.x, v.y, red[w * BN + col].x, red[w * BN + col].y, kLog2e);
+            part[(int64_t)tm * N + n0 + col] = v;
+        }
+    }
+};
+
+// dloss (P - 1 at the target) of a piece of the vocabulary, in 16 bits, as
+// [token][row] and as [row][token].  Tokens up to a multiple of 8 and rows up
+// to the tile's end are written (zeros past the ends): the products that read
+// them walk whole 16-byte groups.
+template <int DT, int WM, int WN, int AM, int AN>
+struct GradEpilogue {
+    uint16_t* dl;          // [n][piece], or null
+    uint16_t* dlt;         // [piece][np], or null
+    int piece, np;         // pitches
+    int64_t v0;            // first vocabulary row of the piece
+    RowState rs;
+    __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int m0, int n0, int M, int N, uint8_t*) const {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
+        const float scale = rs.scale[0];
+#pragma unroll
+        for (int b = 0; b < AN; ++b) {
+            const int t = n0 + wn * AN * 32 + b * 32 + l32;
+            const int64_t target = t < N ? rs.targets[t] - v0 : -1;
+            const float top = t < N ? rs.top[t] : 0.0f, ls = t < N ? rs.ls[t] : 0.0f;
+            const float w = t < N ? rs.w[t] * scale : 0.0f;
+#pragma unroll
+            for (int a = 0; a < AM; ++a)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int v = m0 + (wm * AM + a) * 32 + 8 * q + 4 * hi;
+                    uint16_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float p = exp2_fast(__builtin_fmaf(acc[a][b][4 * q + e] - top, kLog2e, -ls));
+                        if (v + e == target) p -= 1.0f;
+                        o[e] = f32_to_tile<DT>(v + e < M && w != 0.0f ? p * w : 0.0f);
+                    }
+                    if (dl && t < N && v < piece)
+                        *reinterpret_cast<uint2*>(dl + (int64_t)t * piece + v) =
+                            make_uint2(o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16);
+                    if (dlt && t < np && v < piece) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dlt[(int64_t)(v + e) * np + t] = o[e];
+                    }
+                }
+        }
+    }
+};
+
+// Maximum, sum, loss and row weight of every token from its tiles' parts.
+__global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* part, int tiles, int n, int64_t V) {
+    __shared__ float2 red[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int t = blockIdx.x * 64 + lane;
+    float m = -INFINITY, s = 0.0f;
+    if (t < n)
+        for (int i = wave; i < tiles; i += 4) {
+            const float2 v = part[(int64_t)i * n + t];
+            merge(m, s, v.x, v.y, kLog2e);
+        }
+    red[wave][lane] = make_float2(m, s);
+    __syncthreads();
+    if (wave != 0 || t >= n) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) merge(m, s, red[w][lane].x, red[w][lane].y, kLog2e);
+    const int64_t target = rs.targets[t];
+    float ls = __builtin_amdgcn_logf(s);
+    float w = rs.dloss ? rs.dloss[t] : 1.0f;
+    float l = 0.0f;
+    if (target < 0) {
+        w = 0.0f;
+    } else if (target >= V) {
+        ls = l = NAN;
+    } else {
+        l = (m - rs.zt[t]) + kLn2 * ls;
+    }
+    rs.loss[t] = l;
+    rs.top[t] = m;
+    rs.ls[t] = ls;
+    rs.w[t] = w;
+}
+
+// Factor that takes the largest row weight just below 2^15.  Stored gradients of an fp16 model then keep fp16's
+// relative precision whatever the weights' size, and the target's entry, (p - 1) times the weight and often the
+// largest of its row, lies where the type's steps are finest relative to it (equal weights: half the error of the
+// worst factor).
+__global__ void __launch_bounds__(1024) scale_kernel(const float* w, int n, float* scale) {
+    __shared__ float red[16];
+    float m = 0.0f;
+    for (int i = threadIdx.x; i < n; i += 1024) m = fmaxf(m, fabsf(w[i]));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, red[i]);
+    // (the quotient of a weight below 2^-100 would overflow)
+    const bool fits = m > 0x1p-100f && m < INFINITY;
+    scale[0] = fits ? 32760.0f / m : 1.0f;
+    scale[1] = fits ? m / 32760.0f : 1.0f;
+}
+
+// dst[c][r] = src[r][c] for r < R, zero for R <= r < pitch (and for rows whose weight is zero).
+__global__ void __launch_bounds__(256) transpose_kernel(const uint16_t* src, int64_t ld, int R, int C, uint16_t* dst,
+                                                        int pitch, const float* weight) {
+    __shared__ __attribute__((aligned(16))) uint16_t tile[64][72];
+    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int r = r0 + (tid >> 3) + 32 * j, c = c0 + 8 * (tid & 7);
+        u32x4 v{0, 0, 0, 0};
+        if (r < R && c < C && !(weight && weight[r] == 0.0f))
+            v = *reinterpret_cast<const u32x4*>(src + (int64_t)r * ld + c);
+        *reinterpret_cast<u32x4*>(&tile[(tid >> 3) + 32 * j][8 * (tid & 7)]) = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = c0 + (tid >> 3) + 32 * j, r = r0 + 8 * (tid & 7);
+        if (c >= C || r >= pitch) continue;
+        uint16_t o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = tile[8 * (tid & 7) + e][(tid >> 3) + 32 * j];
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = o[2 * e] | (uint32_t)o[2 * e + 1] << 16;
+        *reinterpret_cast<u32x4*>(dst + (int64_t)c * pitch + r) = v;
+    }
+}
+
+hipError_t launch_transpose(const uint16_t* src, int64_t ld, int R, int C, uint16_t* dst, int pitch, const float* weight,
+                            hipStream_t st) {
+    transpose_kernel<<<dim3((unsigned)((pitch + 63) / 64), (unsigned)((C + 63) / 64)), 256, 0, st>>>(src, ld, R, C, dst,
+                                                                                              pitch, weight);
+    return hipGetLastError();
+}
+
+int round_up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
+
+}  // namespace
+
+template <int DT>
+static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W, const RowState& rs, uint16_t* dX,
+                                uint16_t* dW, int n, hipStream_t st) {
+    const int V = L->desc.vocab, F = L->desc.features;
+    hipError_t e;
+    GemmOperands g{};
+    g.zero = L->d_zero;
+    g.A = W;
+    g.lda = F;
+    g.M = V;
+    g.B = X;
+    g.ldb = F;
+    g.N = n;
+    g.K = F;
+    constexpr int WM = 2, WN = 4, AM = 4, AN = 2;
+    if ((e = launch_gemm<DT, WM, WN, AM, AN>(g, StatsEpilogue<WM, WN, AM, AN>{L->d_part, rs}, st)) != hipSuccess) return e;
+    join_kernel<<<(unsigned)((n + 63) / 64), 256, 0, st>>>(rs, L->d_part, (V + 255) / 256, n, V);
+    if ((e = hipGetLastError()) != hipSuccess || (!dX && !dW)) return e;
+    scale_kernel<<<1, 1024, 0, st>>>(rs.w, n, rs.scale);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int np = round_up(n, 8), piece = L->piece;
+    if (dW && (e = launch_transpose(X, F, n, F, L->d_xt, np, rs.w, st)) != hipSuccess) return e;
+    for (int64_t v0 = 0; v0 < V; v0 += piece) {
+        const int rows = (int)std::min<int64_t>(piece, V - v0), rp = round_up(rows, 8);
+        g.A = W + v0 * F;
+        g.lda = g.ldb = F;
+        g.M = rows;
+        g.B = X;
+        g.N = n;
+        g.K = F;
+        GradEpilogue<DT, WM, WN, AM, AN> ge{dX ? L->d_dl : nullptr, dW ? L->d_dlt : nullptr, piece, np, v0, rs};
+        if ((e = launch_gemm<DT, WM, WN, AM, AN>(g, ge, st)) != hipSuccess) return e;
+        if (dX) {
+            if ((e = launch_transpose(W + v0 * F, F, rows, F, L->d_wt, piece, nullptr, st)) != hipSuccess) return e;
+            GemmOperands d = g;
+            d.A = L->d_dl;
+            d.B = L->d_wt;
+            d.lda = d.ldb = piece;
+            d.M = n;
+            d.N = F;
+            d.K = rp;
+            const bool last = v0 + piece >= V;
+            StoreEpilogue<DT, WM, WN, AM, AN> se{last ? dX : nullptr, L->d_dx, F, v0 == 0, rs.scale + 1};
+            if ((e = launch_gemm<DT, WM, WN, AM, AN>(d, se, st)) != hipSuccess) return e;
+        }
+        if (dW) {
+            GemmOperands d = g;
+            d.A = L->d_dlt;
+            d.B = L->d_xt;
+            d.lda = d.ldb = np;
+            d.M = rows;
+            d.N = F;
+            d.K = np;
+            StoreEpilogue<DT, WM, WN, AM, AN> se{dW + v0 * F, nullptr, F, 1, rs.scale + 1};
+            if ((e = launch_gemm<DT, WM, WN, AM, AN>(d, se, st)) != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+template <int DT>
+static hipError_t distill(const DistillArgs& a, hipStream_t st) {
+    distill_kernel<DT, 512><<<(unsigned)std::min(a.n, kMaxRowBlocks), 512, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace aq
+
+namespace {
+
+void free_loss(aq_loss* L) {
+    void* ptrs[] = {L->d_zero, L->d_part, L->d_row, L->d_dl, L->d_dlt, L->d_wt, L->d_xt, L->d_dx};
+    for (void* p : ptrs)
+        if (p) (void)hipFree(p);
+    delete L;
+}
+
+template <typename T>
+aq_status alloc(T** p, size_t bytes, const char* what) {
+    if (*p) return AQ_OK;
+    const hipError_t e = hipMalloc(reinterpret_cast<void**>(p), bytes);
+    if (e == hipSuccess) return AQ_OK;
+    *p = nullptr;
+    return api_hip_fail(e, what);
+}
+
+// The gradients' workspace (the first call that asks for one allocates it).
+aq_status grad_workspace(aq_loss* L, bool dx, bool dw) {
+    const size_t n = (size_t)(L->desc.max_tokens + 7) / 8 * 8, F = (size_t)L->desc.features, P = (size_t)L->piece;
+    aq_status s = AQ_OK;
+    if (dx) {
+        s = alloc(&L->d_dl, n * P * 2, "gradient workspace");
+        if (s == AQ_OK) s = alloc(&L->d_wt, F * P * 2, "gradient workspace");
+        if (s == AQ_OK && L->piece < L->desc.vocab) s = alloc(&L->d_dx, n * F * 4, "gradient workspace");
+    }
+    if (s == AQ_OK && dw) s = alloc(&L->d_dlt, n * P * 2, "gradient workspace");
+    if (s == AQ_OK && dw) s = alloc(&L->d_xt, n * F * 2, "gradient workspace");
+    return s;
+}
+
+bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+aq_status check_call(const aq_loss* L, int64_t n) {
+    if (n < 1) return api_fail(AQ_ERR_INVALID_ARGUMENT, "n must be >= 1");
+    if (n > L->desc.max_tokens) return api_fail(AQ_ERR_INVALID_ARGUMENT, "tokens exceed max_tokens");
+    int dev = 0;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return api_hip_fail(e, "hipGetDevice");
+    if (dev != L->device) return api_fail(AQ_ERR_INVALID_ARGUMENT, "the losses were created on another device");
+    return AQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
+    if (out) *out = nullptr;
+    if (!desc || !out) return api_fail(AQ_ERR_INVALID_ARGUMENT, "null pointer argument");
+    if (desc->vocab < 1) return api_fail(AQ_ERR_INVALID_ARGUMENT, "vocab must be >= 1");
+    if (desc->vocab > (1 << 30)) return api_fail(AQ_ERR_UNSUPPORTED, "vocab above 2^30");
+    if (desc->features < 0) return api_fail(AQ_ERR_INVALID_ARGUMENT, "features must be >= 0");
+    if (desc->dtype != AQ_F32 && desc->dtype != AQ_F16 && desc->dtype != AQ_BF16)
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "dtype must be F32, F16 or BF16");
+    if (desc->max_tokens < 1) return api_fail(AQ_ERR_INVALID_ARGUMENT, "max_tokens must be >= 1");
+    if (desc->max_tokens > (1 << 24)) return api_fail(AQ_ERR_UNSUPPORTED, "max_tokens above 2^24");
+    if (desc->features && desc->dtype == AQ_F32)
+        return api_fail(AQ_ERR_UNSUPPORTED, "the cross entropy takes fp16 or bf16 inputs and head weights");
+    if (desc->features % 8 != 0) return api_fail(AQ_ERR_UNSUPPORTED, "features must be a multiple of 8");
+    if (desc->features > (1 << 20)) return api_fail(AQ_ERR_UNSUPPORTED, "features above 2^20");
+    int ndev = 0;
+    hipError_t e = hipGetDeviceCount(&ndev);
+    if (e != hipSuccess || ndev < 1) return api_fail(AQ_ERR_DEVICE, "no HIP device available");
+    aq_loss* L = new (std::nothrow) aq_loss();
+    if (!L) return api_fail(AQ_ERR_OUT_OF_MEMORY, "host allocation");
+    L->desc = *desc;
+    e = hipGetDevice(&L->device);
+    if (e != hipSuccess) {
+        delete L;
+        return api_hip_fail(e, "hipGetDevice");
+    }
+    if (desc->features) {
+        // a piece's gradient and its transposed head rows take at most 128 MiB each
+        const int64_t most = (int64_t(64) << 20) / std::max<int64_t>(desc->max_tokens, desc->features);
+        const int64_t pieces = (desc->vocab + std::max<int64_t>(most, 256) - 1) / std::max<int64_t>(most, 256);
+        L->piece = (int)(((desc->vocab + pieces - 1) / pieces + 255) / 256 * 256);
+        const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 255) / 256;
+        aq_status s = alloc(&L->d_zero, 256, "zero block");
+        if (s == AQ_OK) s = alloc(&L->d_part, tiles * n * sizeof(float2), "row statistics");
+        if (s == AQ_OK) s = alloc(&L->d_row, (4 * n + 2) * sizeof(float), "row state");
+        if (s == AQ_OK && (e = hipMemset(L->d_zero, 0, 256)) != hipSuccess) s = api_hip_fail(e, "zero block");
+        if (s == AQ_OK && (e = hipDeviceSynchronize()) != hipSuccess) s = api_hip_fail(e, "zero block");
+        if (s != AQ_OK) {
+            free_loss(L);
+            return s;
+        }
+    }
+    *out = L;
+    return AQ_OK;
+}
+
+aq_status aq_loss_cross_entropy(aq_loss* L, const void* X, const void* W, const int64_t* targets, const float* dloss,
+                                float* loss, void* dX, void* dW, int64_t n, void* stream) {
+    if (!L || !X || !W || !targets || !loss) return api_fail(AQ_ERR_INVALID_ARGUMENT, "null pointer argument");
+    if (!L->desc.features) return api_fail(AQ_ERR_INVALID_ARGUMENT, "created without features: distillation only");
+    if (misaligned(X, 16) || misaligned(W, 16) || misaligned(dX, 16) || misaligned(dW, 16))
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "X, W, dX and dW must be 16-byte aligned");
+    if (misaligned(targets, 8)) return api_fail(AQ_ERR_INVALID_ARGUMENT, "targets must be 8-byte aligned");
+    if (misaligned(dloss, 4) || misaligned(loss, 4))
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "dloss and loss must be 4-byte aligned");
+    aq_status s = check_call(L, n);
+    if (s != AQ_OK) return s;
+    if (dX || dW) {
+        s = grad_workspace(L, dX != nullptr, dW != nullptr);
+        if (s != AQ_OK) return s;
+    }
+    const int64_t mt = L->desc.max_tokens;
+    const aq::RowState rs{targets, dloss, L->d_row, L->d_row + mt, L->d_row + 2 * mt, L->d_row + 3 * mt, loss,
+                          L->d_row + 4 * mt};
+    const auto st = static_cast<hipStream_t>(stream);
+    const auto x = static_cast<const uint16_t*>(X), w = static_cast<const uint16_t*>(W);
+    const auto dx = static_cast<uint16_t*>(dX), dw = static_cast<uint16_t*>(dW);
+    const hipError_t e = L->desc.dtype == AQ_F16 ? aq::cross_entropy<AQ_F16>(L, x, w, rs, dx, dw, (int)n, st)
+                                                 : aq::cross_entropy<AQ_BF16>(L, x, w, rs, dx, dw, (int)n, st);
+    return e == hipSuccess ? AQ_OK : api_hip_fail(e, "cross entropy launch");
+}
+
+aq_status aq_loss_distill(aq_loss* L, const void* logits, const int32_t* ids, const void* teacher, int32_t top,
+                          float temperature, const float* dloss, float* loss, void* dlogits, int64_t n, void* stream) {
+    if (!L || !logits || !ids || !teacher || !loss) return api_fail(AQ_ERR_INVALID_ARGUMENT, "null pointer argument");
+    if (top < 1) return api_fail(AQ_ERR_INVALID_ARGUMENT, "top must be >= 1");
+    if (top > aq::kMaxTop) return api_fail(AQ_ERR_UNSUPPORTED, "top above 1024");
+    if (!(temperature > 0.0f) || !std::isfinite(temperature))
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "temperature must be positive and finite");
+    const unsigned b = L->desc.dtype == AQ_F32 ? 4 : 2;
+    if (misaligned(logits, 16) || misaligned(dlogits, 16))
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "logits and dlogits must be 16-byte aligned");
+    if (misaligned(ids, 4) || misaligned(teacher, b) || misaligned(dloss, 4) || misaligned(loss, 4))
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "ids, teacher, dloss and loss must be aligned to their values");
+    const aq_status s = check_call(L, n);
+    if (s != AQ_OK) return s;
+    const aq::DistillArgs a{logits, ids, teacher, dloss, loss, dlogits, n, L->desc.vocab, top, aq::kLog2e / temperature,
+                            temperature};
+    const auto st = static_cast<hipStream_t>(stream);
+    const hipError_t e = L->desc.dtype == AQ_F32   ? aq::distill<AQ_F32>(a, st)
+                         : L->desc.dtype == AQ_F16 ? aq::distill<AQ_F16>(a, st)
+                                                   : aq::distill<AQ_BF16>(a, st);
+    return e == hipSuccess ? AQ_OK : api_hip_fail(e, "distillation launch");
+}
+
+aq_status aq_loss_destroy(aq_loss* L) {
+    if (!L) return AQ_OK;
+    const hipError_t e = hipDeviceSynchronize();
+    free_loss(L);
+    return e == hipSuccess ? AQ_OK : api_hip_fail(e, "destroy");
+}
+
+}  // extern "C"
