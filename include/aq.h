@@ -387,12 +387,17 @@ aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* 
 
 /*
  * Forward Y = X * W^T on `stream`; asynchronous, allocates nothing and never
- * synchronises.  Weights are not rounded: the integers q - z are multiplied
- * with the inputs exactly, sums are fp32, and each group's sum is scaled.
+ * synchronises.  Weights are not rounded: the codes are multiplied with the
+ * inputs exactly, sums are fp32, and each group's sum is scaled, its zero
+ * point times the sum of the group's inputs taken off (inputs so large that 15
+ * times a group's sum passes fp32 give infinities or NaN).
  * Summation orders are fixed for each n: repeated calls give identical bits.
  *   X   device [n][in_features] in desc->dtype; 16-byte aligned
  *   Y   device [n][out_features] in desc->y_dtype; 16-byte aligned
  *   n   1 <= n <= max_tokens
+ * Above 64 tokens a call uses the layer's workspace (the inputs' group sums,
+ * 16 bytes per token and group, and at most 32 MiB of partial sums, allocated
+ * with the layer): serialise such calls on one stream.
  * The layer's device has to be the current one (AQ_ERR_INVALID_ARGUMENT).
  */
 aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void* stream);

@@ -8,13 +8,15 @@
 // 16 bytes of lane l = 16 * o + r holding row r's inputs 32 * s + 8 * o + e of
 // step s (word s, value e): word s of all lanes is the B operand of one
 // v_mfma_f32_16x16x32 once its eight codes are widened, and a wave reads a tile
-// as 64 consecutive 16-byte loads.  Value 2 p of a word is its nibble p and
-// value 2 p + 1 its nibble p + 4, so that one shift and mask leaves a pair in
-// the two halves of a register.  Scales and zero points: [row tile][group][16].
+// as 64 consecutive 16-byte loads.  Byte b of a word holds value b in its lower
+// half and value 4 + b in its upper half.  Scales and zero points:
+// [row tile][group][16].
 //
-// q - z is an integer of five bits, exact in fp16 and bf16: the matrix cores
-// multiply it with the unrounded inputs, and the scale is applied to each
-// group's fp32 sum.  No weight is rounded.
+// The products run on the codes themselves: integers below 16, exact in fp16
+// and bf16, times the unrounded inputs, in fp32.  With S_j the sum of group j's
+// inputs,
+//     Y[t][i] = sum_j s[i][j] * (sum_{k in j} q[i][k] x[t][k] - z[i][j] * S_j[t]),
+// so each group's fp32 sum is scaled once and no weight is ever rounded.
 #include <algorithm>
 #include <new>
 
@@ -32,6 +34,10 @@ struct aq_usq {
     uint16_t* d_scales;
     uint8_t* d_zeros;      // null: every zero point is 8
     uint8_t* d_zero;       // 256 zero bytes
+    // more than 64 tokens: group sums of the inputs, and a K split's partial sums
+    uint16_t* d_sums;
+    float* d_part;
+    int sum_groups;
     // input gradient, allocated by its first call
     uint16_t* d_wt;        // [slab][Cp] decoded weights of a slab of inputs, transposed
     uint16_t* d_dy;        // [max_tokens][Cp] output gradient with rows of whole 16-byte groups (C_out % 8 != 0)
@@ -52,6 +58,12 @@ struct UsqArgs {
     int n, K, C_out;
     int nchunk, groups;
     int per;               // group >= 128: chunks a group
+    // many tokens
+    const uint8_t* zero;   // 16 zero bytes
+    uint16_t* sums;        // group sums of the inputs
+    int sum_groups;        // groups a row of it holds
+    float* part;           // K split: [split][n][C_out] partial sums, else null
+    int cps;               // chunks a split
 };
 
 // Packed codes as the caller has them ([C_out][K / 2], the lower half first) into the device layout.
@@ -67,7 +79,7 @@ __global__ void __launch_bounds__(256) usq_pack_kernel(const uint8_t* src, uint3
     uint32_t v = 0, o = 0;
     if (i < C_out && k < K) v = *reinterpret_cast<const uint32_t*>(src + i * (K / 2) + k / 2);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) o |= ((v >> (8 * p)) & 15u) << (4 * p) | ((v >> (8 * p + 4)) & 15u) << (4 * p + 16);
+    for (int e = 0; e < 8; ++e) o |= ((v >> (4 * e)) & 15u) << (8 * (e & 3) + 4 * (e >> 2));
     dst[w] = o;
 }
 
@@ -81,30 +93,25 @@ __global__ void __launch_bounds__(256) usq_groups_kernel(const T* src, T* dst, i
     dst[w] = i < C_out && j < G ? src[i * G + j] : T(0);
 }
 
-// The eight codes of a word as 16-bit integers in value order.
+// The eight codes of a word as 16-bit floats in value order.  A byte b below 16
+// is the fp8 (e4m3) number b * 2^-9, subnormal or not, so the conversion from
+// fp8 with the scale 2^9 widens two codes an instruction, exactly (all sixteen
+// codes checked): 7 instructions a word.  Through fp32, byte by byte, it
+// takes 15.
 template <int DT>
 __device__ __forceinline__ u32x4 widen_codes(uint32_t w) {
+    const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
     u32x4 o;
     if constexpr (DT == AQ_F16) {
-        // 0x6400 | q is 1024 + q
-        const half2v off{(_Float16)-1024.0f, (_Float16)-1024.0f};
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const uint32_t v = ((w >> (4 * p)) & 0x000f000fu) | 0x64006400u;
-            o[p] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, v) + off);
-        }
+        o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, false));
+        o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, true));
+        o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, false));
+        o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, true));
     } else {
-        const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
-        // an integer below 16 fills the upper half of its fp32 alone
-        auto pair = [](uint32_t b, int x, int y) {
-            const uint32_t fx = __float_as_uint((float)((b >> (8 * x)) & 255u));
-            const uint32_t fy = __float_as_uint((float)((b >> (8 * y)) & 255u));
-            return __builtin_amdgcn_perm(fy, fx, 0x07060302u);
-        };
-        o[0] = pair(lo, 0, 2);
-        o[1] = pair(hi, 0, 2);
-        o[2] = pair(lo, 1, 3);
-        o[3] = pair(hi, 1, 3);
+        o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, false));
+        o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, true));
+        o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, false));
+        o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, true));
     }
     return o;
 }
@@ -131,81 +138,376 @@ __device__ __forceinline__ void store_y3(void* Y, int y_dtype, int64_t i, float 
     else static_cast<uint16_t*>(Y)[i] = f32_to_bf16(v);
 }
 
-// 16 output rows x 16 tokens a workgroup; its waves share K chunk by chunk and
-// add their sums in LDS in wave order.  SG: steps of 32 inputs a scale group
-// (group 32, 64, and 128 or more).  The zero point leaves through the group
-// sum of the inputs, z * sum_k x, which a product with ones delivers in the
-// accumulators' own layout.
-template <int DT, int SG>
+// ---- few tokens ----
+
+constexpr int kFewTokens = 64;
+
+// 16 output rows x 16 NT tokens a workgroup; its waves share K chunk by chunk
+// and add their sums in LDS in wave order.  SG: steps of 32 inputs a scale
+// group (group 32, 64, and 128 or more).  S_j comes from a product with ones,
+// which delivers it in the accumulators' own layout.
+template <int DT, int SG, int NT>
 __global__ void __launch_bounds__(512) usq_few_kernel(UsqArgs a) {
-    __shared__ floatx4 red[8][64];
+    __shared__ floatx4 red[8][NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
     const int l16 = lane & 15, o = lane >> 4;
-    const int rt = blockIdx.x, t0 = blockIdx.y * 16;
-    const int t = min(t0 + l16, a.n - 1);
-    const uint16_t* x = a.X + (int64_t)t * a.K + 8 * o;
+    const int rt = blockIdx.x;
+    const uint16_t* x[NT];
+#pragma unroll
+    for (int m = 0; m < NT; ++m) x[m] = a.X + (int64_t)min(16 * m + l16, a.n - 1) * a.K + 8 * o;
     const u32x4* codes = reinterpret_cast<const u32x4*>(a.codes) + (int64_t)rt * a.nchunk * 64 + lane;
     const int64_t srow = (int64_t)rt * a.groups * 16 + l16;
     const uint32_t one = DT == AQ_BF16 ? 0x3f803f80u : 0x3c003c00u;
     const u32x4 ones{one, one, one, one};
-    floatx4 acc{0.0f, 0.0f, 0.0f, 0.0f};
+    floatx4 acc[NT];
+#pragma unroll
+    for (int m = 0; m < NT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     for (int c = wave; c < a.nchunk; c += waves) {
         const u32x4 w = codes[(int64_t)c * 64];
-        u32x4 xv[4];
+        u32x4 xv[4][NT];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int k = c * 128 + 32 * s;
-            xv[s] = u32x4{0, 0, 0, 0};
-            if (k + 8 * o < a.K) xv[s] = *reinterpret_cast<const u32x4*>(x + k);
+#pragma unroll
+            for (int m = 0; m < NT; ++m) {
+                xv[s][m] = u32x4{0, 0, 0, 0};
+                if (k + 8 * o < a.K) xv[s][m] = *reinterpret_cast<const u32x4*>(x[m] + k);
+            }
         }
 #pragma unroll
         for (int g = 0; g < 4 / SG; ++g) {
             const int j = SG == 4 ? c / a.per : c * (4 / SG) + g;
             const float sc = widen16<DT>(a.scales[srow + (int64_t)j * 16]);
             const float z = a.zeros ? (float)a.zeros[srow + (int64_t)j * 16] : 8.0f;
-            floatx4 d{0.0f, 0.0f, 0.0f, 0.0f}, xs{0.0f, 0.0f, 0.0f, 0.0f};
+            floatx4 d[NT], xs[NT];
+#pragma unroll
+            for (int m = 0; m < NT; ++m) d[m] = xs[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int s = g * SG; s < (g + 1) * SG; ++s) {
-                d = mfma16<DT>(xv[s], widen_codes<DT>(w[s]), d);
-                xs = mfma16<DT>(xv[s], ones, xs);
+                const u32x4 q = widen_codes<DT>(w[s]);
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    d[m] = mfma16<DT>(xv[s][m], q, d[m]);
+                    xs[m] = mfma16<DT>(xv[s][m], ones, xs[m]);
+                }
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(sc, __builtin_fmaf(-z, xs[r], d[r]), acc[r]);
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    acc[m][r] = __builtin_fmaf(sc, __builtin_fmaf(-z, xs[m][r], d[m][r]), acc[m][r]);
         }
     }
-    red[wave][lane] = acc;
-    __syncthreads();
-    if (wave != 0) return;
-    for (int w = 1; w < waves; ++w) acc += red[w][lane];
-    const int i = rt * 16 + l16;
-    if (i >= a.C_out) return;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int tok = t0 + 4 * o + r;
-        if (tok < a.n) store_y3(a.Y, a.y_dtype, (int64_t)tok * a.C_out + i, acc[r]);
+    for (int m = 0; m < NT; ++m) red[wave][m][lane] = acc[m];
+    __syncthreads();
+    const int i = rt * 16 + l16;
+    for (int m = wave; m < NT; m += waves) {
+        floatx4 v = red[0][m][lane];
+        for (int w = 1; w < waves; ++w) v += red[w][m][lane];
+        if (i >= a.C_out) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int tok = 16 * m + 4 * o + r;
+            if (tok < a.n) store_y3(a.Y, a.y_dtype, (int64_t)tok * a.C_out + i, v[r]);
+        }
     }
 }
 
 template <int DT, int SG>
 hipError_t launch_few(const UsqArgs& a, hipStream_t st) {
     const int waves = std::min(8, a.nchunk);
-    constexpr int kMost = 65535 * 16;          // tokens of a launch
-    for (int t0 = 0; t0 < a.n; t0 += kMost) {
-        UsqArgs p = a;
-        p.n = std::min(kMost, a.n - t0);
-        p.X += (int64_t)t0 * a.K;
-        p.Y = static_cast<uint8_t*>(a.Y) + (int64_t)t0 * a.C_out * (a.y_dtype == AQ_F32 ? 4 : 2);
-        usq_few_kernel<DT, SG><<<dim3((unsigned)((a.C_out + 15) / 16), (unsigned)((p.n + 15) / 16)), waves * 64, 0, st>>>(p);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)((a.C_out + 15) / 16));
+    if (a.n <= 16) usq_few_kernel<DT, SG, 1><<<grid, waves * 64, 0, st>>>(a);
+    else if (a.n <= 32) usq_few_kernel<DT, SG, 2><<<grid, waves * 64, 0, st>>>(a);
+    else usq_few_kernel<DT, SG, 4><<<grid, waves * 64, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+// ---- many tokens ----
+
+// Group sums of the inputs, S[t][j], as three bf16 pieces that add up to the
+// fp32 sum: [n][groups rounded up to 2][8] = {h, m, l, h, m, l, 0, 0}.
+template <int DT>
+__global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
+    // eight lanes a group, 16-byte loads
+    const int gp = a.sum_groups;
+    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int part = threadIdx.x & 7;
+    if (id >= (int64_t)a.n * gp) return;
+    const int64_t t = id / gp;
+    const int j = (int)(id - t * gp);
+    float s = 0.0f;
+    for (int k = j * group + 8 * part; k < min((j + 1) * group, a.K); k += 64) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(a.X + t * a.K + k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += widen16<DT>((uint16_t)v[e]) + widen16<DT>((uint16_t)(v[e] >> 16));
     }
-    return hipSuccess;
+    s += __shfl_xor(s, 1);
+    s += __shfl_xor(s, 2);
+    s += __shfl_xor(s, 4);
+    if (part != 0) return;
+    const uint32_t h = f32_to_bf16(s);
+    const float r1 = s - bf16_to_f32((uint16_t)h);
+    const uint32_t m = f32_to_bf16(r1);
+    const uint32_t l = f32_to_bf16(r1 - bf16_to_f32((uint16_t)m));
+    reinterpret_cast<u32x4*>(a.sums)[id] = u32x4{h | m << 16, l | h << 16, m | l << 16, 0u};
+}
+
+// A 2 x 2 grid of waves on a (64 AM) x (64 AN) tile of tokens x output rows;
+// wave tiles of 32 AM x 32 AN in blocks of v_mfma_f32_32x32x16 (D rows: tokens,
+// columns: output rows, so that a lane has one scale a block and group).
+//  * The tile's tokens reach LDS 128 inputs at a time through direct-to-LDS
+//    loads, in two stages (slots permuted as in gemm_mainloop, sixteen a row).
+//  * Weights go from the code tiles to registers, are widened there once a
+//    chunk, and serve all of the wave's tokens; no LDS traffic.
+//  * A group's sum accumulates on its own (two token blocks at a time, four
+//    independent chains) and is scaled into the running sum.
+//  * The zero points come first: -s z times the group sums is a product over
+//    groups, of s z in two bf16 pieces (15 bits at most, exact) and the sums in
+//    three, six of the eight values a lane holds for one group.
+// SG: steps of 16 inputs a group within a chunk.
+template <int DT, int SG, int AM, int AN>
+__global__ void __launch_bounds__(256, AM == 4 ? 1 : 2) usq_gemm_kernel(UsqArgs a) {
+    constexpr int BM = 64 * AM, BN = 64 * AN, AP = AM < 2 ? 1 : 2;
+    constexpr int STAGE = BM * 256, LOADS = BM * 16 / 256;
+    extern __shared__ __attribute__((aligned(16))) uint8_t usq_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave & 1, wn = wave >> 1, l32 = lane & 31, hi = lane >> 5;
+    // XCD-aware order: each XCD takes a contiguous run, token tiles fastest in bands of eight
+    const int tiles_m = (a.n + BM - 1) / BM, tiles_n = (a.C_out + BN - 1) / BN;
+    int tm, tn, z;
+    {
+        const int nwg = (int)gridDim.x, h = (int)blockIdx.x;
+        const int xcd = h & 7, per = nwg >> 3, rem = nwg & 7;
+        int w = xcd * per + min(xcd, rem) + (h >> 3);
+        z = w / (tiles_m * tiles_n);
+        w -= z * tiles_m * tiles_n;
+        const int band = w / (8 * tiles_n), rows = min(8, tiles_m - 8 * band);
+        const int in = w - band * 8 * tiles_n;
+        tn = in / rows;
+        tm = 8 * band + in - tn * rows;
+    }
+    const int m0 = tm * BM, n0 = tn * BN;
+    const int c_beg = z * a.cps, c_end = min(a.nchunk, c_beg + a.cps);
+
+    // ---- staging of the tokens ----
+    const int r0 = tid >> 4, slot = (tid & 15) ^ (r0 & 7);
+    const uint16_t* px[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) px[j] = a.X + (int64_t)min(m0 + r0 + 16 * j, a.n - 1) * a.K + 8 * slot;
+    auto issue = [&](int chunk, uint8_t* st) {
+        const int k0 = chunk * 128;
+        const bool in = k0 + 8 * slot < a.K;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j)
+            lds_dma16(in ? reinterpret_cast<const uint8_t*>(px[j] + k0) : a.zero, st + (j * 256 + wave * 64) * 16);
+    };
+
+    // ---- weights: this lane's column of each block, two 16-byte loads a chunk ----
+    const u32x4* pc[AN];
+    int64_t srow[AN];
+#pragma unroll
+    for (int b = 0; b < AN; ++b) {
+        const int i = n0 + (wn * AN + b) * 32 + l32;
+        const int rt = min(i, a.C_out - 1) >> 4;       // rows past the end: any tile, never stored
+        pc[b] = reinterpret_cast<const u32x4*>(a.codes) + (int64_t)rt * a.nchunk * 64 + 16 * hi + (i & 15);
+        srow[b] = (int64_t)rt * a.groups * 16 + (i & 15);
+    }
+    constexpr int GPC = 8 / SG;                        // groups a chunk (1 for groups of 128 and more)
+    u32x4 wc[AN][2];
+    uint16_t sc[AN][GPC];
+    auto load_weights = [&](int chunk) {
+#pragma unroll
+        for (int b = 0; b < AN; ++b) {
+            wc[b][0] = pc[b][(int64_t)chunk * 64];
+            wc[b][1] = pc[b][(int64_t)chunk * 64 + 32];
+#pragma unroll
+            for (int g = 0; g < GPC; ++g) {
+                const int j = GPC == 1 ? chunk / a.per : chunk * GPC + g;
+                sc[b][g] = a.scales[srow[b] + (int64_t)j * 16];
+            }
+        }
+    };
+
+    floatx16 acc[AM][AN];
+#pragma unroll
+    for (int x = 0; x < AM; ++x)
+#pragma unroll
+        for (int b = 0; b < AN; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[x][b][r] = 0.0f;
+
+    issue(c_beg, usq_lds);
+    load_weights(c_beg);
+    // ---- zero points of the groups that begin in this split's chunks ----
+    {
+        const int j_beg = GPC == 1 ? (c_beg + a.per - 1) / a.per : c_beg * GPC;
+        const int j_end = GPC == 1 ? (c_end + a.per - 1) / a.per : c_end * GPC;
+        const u32x4* ps[AM];
+#pragma unroll
+        for (int x = 0; x < AM; ++x)
+            ps[x] = reinterpret_cast<const u32x4*>(a.sums) +
+                    (int64_t)min(m0 + (wm * AM + x) * 32 + l32, a.n - 1) * a.sum_groups;
+#pragma unroll 2
+        for (int j0 = j_beg; j0 < j_end; j0 += 2) {
+            const int j = min(j0 + hi, j_end - 1);
+            const bool live = j0 + hi < j_end;
+            u32x4 fs[AM];
+#pragma unroll
+            for (int x = 0; x < AM; ++x) {
+                fs[x] = ps[x][min(j, a.sum_groups - 1)];
+                if (!live) fs[x] = u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int b = 0; b < AN; ++b) {
+                const int64_t at = srow[b] + (int64_t)j * 16;
+                const float v = -widen16<DT>(a.scales[at]) * (a.zeros ? (float)a.zeros[at] : 8.0f);
+                const uint32_t h = f32_to_bf16(v), l = f32_to_bf16(v - bf16_to_f32((uint16_t)h));
+                const u32x4 fz{h | h << 16, h | l << 16, l | l << 16, 0u};
+#pragma unroll
+                for (int x = 0; x < AM; ++x) acc[x][b] = mfma_gemm<AQ_BF16>(fs[x], fz, acc[x][b]);
+            }
+        }
+    }
+
+    const uint32_t arow = (uint32_t)(wm * AM * 32 + l32) * 256u;
+    for (int c = c_beg; c < c_end; ++c) {
+        const uint8_t* st = usq_lds + ((c - c_beg) & 1) * STAGE;
+        wait_vmcnt<0>();
+        lds_barrier();
+        u32x4 q[AN][8];
+        float s32[AN][GPC];
+#pragma unroll
+        for (int b = 0; b < AN; ++b) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) q[b][u] = widen_codes<DT>(wc[b][u & 1][u >> 1]);
+#pragma unroll
+            for (int g = 0; g < GPC; ++g) s32[b][g] = widen16<DT>(sc[b][g]);
+        }
+        if (c + 1 < c_end) {
+            issue(c + 1, usq_lds + ((c + 1 - c_beg) & 1) * STAGE);
+            load_weights(c + 1);
+        }
+#pragma unroll
+        for (int x0 = 0; x0 < AM; x0 += AP)
+#pragma unroll
+            for (int g = 0; g < GPC; ++g) {
+                floatx16 d[AP][AN];
+#pragma unroll
+                for (int u = g * SG; u < (g + 1) * SG; ++u) {
+                    u32x4 xf[AP];
+#pragma unroll
+                    for (int x = 0; x < AP; ++x)
+                        xf[x] = *reinterpret_cast<const u32x4*>(st + arow + (x0 + x) * 8192 +
+                                                                (((2 * u + hi) ^ (l32 & 7)) * 16));
+#pragma unroll
+                    for (int x = 0; x < AP; ++x)
+#pragma unroll
+                        for (int b = 0; b < AN; ++b) {
+                            if (u == g * SG) {
+                                floatx16 zero;
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+                                d[x][b] = mfma_gemm<DT>(xf[x], q[b][u], zero);
+                            } else {
+                                d[x][b] = mfma_gemm<DT>(xf[x], q[b][u], d[x][b]);
+                            }
+                        }
+                }
+#pragma unroll
+                for (int x = 0; x < AP; ++x)
+#pragma unroll
+                    for (int b = 0; b < AN; ++b)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            acc[x0 + x][b][r] = __builtin_fmaf(s32[b][g], d[x][b][r], acc[x0 + x][b][r]);
+            }
+    }
+
+    float* part = a.part ? a.part + (int64_t)z * a.n * a.C_out : nullptr;
+#pragma unroll
+    for (int x = 0; x < AM; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int t = m0 + (wm * AM + x) * 32 + gemm_row(r, hi);
+            if (t >= a.n) continue;
+#pragma unroll
+            for (int b = 0; b < AN; ++b) {
+                const int i = n0 + (wn * AN + b) * 32 + l32;
+                if (i >= a.C_out) continue;
+                if (part) part[(int64_t)t * a.C_out + i] = acc[x][b][r];
+                else store_y3(a.Y, a.y_dtype, (int64_t)t * a.C_out + i, acc[x][b][r]);
+            }
+        }
+}
+
+// Y = sum over the K splits, in split order.
+__global__ void __launch_bounds__(256) usq_join_kernel(const float* part, int splits, int64_t count, void* Y, int y_dtype) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        float v = part[i];
+        for (int z = 1; z < splits; ++z) v += part[z * count + i];
+        store_y3(Y, y_dtype, i, v);
+    }
+}
+
+struct UsqPlan {
+    int am;                // token blocks of 64 a tile
+    int tiles, cps, splits;
+};
+
+// Tiles of 256 tokens once they fill the chip, else of 128; K split over
+// workgroups until they do.
+UsqPlan usq_plan(int64_t n, int C_out, int nchunk) {
+    UsqPlan p;
+    const int64_t tn = (C_out + 127) / 128;
+    p.am = (n + 255) / 256 * tn >= 256 ? 4 : 2;
+    const int64_t tiles = (n + 64 * p.am - 1) / (64 * p.am) * tn;
+    p.tiles = (int)tiles;
+    const int most = std::max(1, nchunk / 4);
+    int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / tiles));
+    if (p.am == 4) splits = 1;
+    p.cps = (nchunk + splits - 1) / splits;
+    p.splits = (nchunk + p.cps - 1) / p.cps;
+    return p;
+}
+
+template <int DT, int SG, int AM, int AN>
+hipError_t launch_usq_gemm(const UsqArgs& a, int grid, hipStream_t st) {
+    constexpr size_t lds = 2 * 64 * AM * 256;
+    auto kern = usq_gemm_kernel<DT, SG, AM, AN>;
+    const hipError_t e = ensure_dynamic_lds((const void*)kern, lds);
+    if (e != hipSuccess) return e;
+    kern<<<(unsigned)grid, 256, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int DT, int SG>
+hipError_t launch_many(UsqArgs a, int group, float* part, hipStream_t st) {
+    const UsqPlan p = usq_plan(a.n, a.C_out, a.nchunk);
+    const int64_t sums = (int64_t)a.n * a.sum_groups;
+    usq_sums_kernel<DT><<<(unsigned)((sums * 8 + 255) / 256), 256, 0, st>>>(a, group);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.cps = p.cps;
+    a.part = p.splits > 1 ? part : nullptr;
+    e = p.am == 4 ? launch_usq_gemm<DT, SG, 4, 2>(a, p.tiles * p.splits, st)
+                  : launch_usq_gemm<DT, SG, 2, 2>(a, p.tiles * p.splits, st);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t count = (int64_t)a.n * a.C_out;
+    usq_join_kernel<<<(unsigned)std::min<int64_t>((count + 255) / 256, 4096), 256, 0, st>>>(part, p.splits, count, a.Y,
+                                                                                           a.y_dtype);
+    return hipGetLastError();
 }
 
 template <int DT>
-hipError_t launch_usq_forward(const UsqArgs& a, int group, hipStream_t st) {
-    return group == 32 ? launch_few<DT, 1>(a, st) : group == 64 ? launch_few<DT, 2>(a, st) : launch_few<DT, 4>(a, st);
+hipError_t launch_usq_forward(const UsqArgs& a, int group, float* part, hipStream_t st) {
+    if (a.n <= kFewTokens)
+        return group == 32 ? launch_few<DT, 1>(a, st) : group == 64 ? launch_few<DT, 2>(a, st) : launch_few<DT, 4>(a, st);
+    return group == 32   ? launch_many<DT, 2>(a, group, part, st)
+           : group == 64 ? launch_many<DT, 4>(a, group, part, st)
+                         : launch_many<DT, 8>(a, group, part, st);
 }
 
 // ---- input gradient ----
@@ -297,7 +599,7 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
 namespace {
 
 void free_usq(aq_usq* L) {
-    void* ptrs[] = {L->d_codes, L->d_scales, L->d_zeros, L->d_zero, L->d_wt, L->d_dy};
+    void* ptrs[] = {L->d_codes, L->d_scales, L->d_zeros, L->d_zero, L->d_sums, L->d_part, L->d_wt, L->d_dy};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     delete L;
@@ -325,6 +627,18 @@ aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t
     if (s == AQ_OK) s = alloc(&L->d_scales, (size_t)count * 2, "scales");
     if (s == AQ_OK && zeros) s = alloc(&L->d_zeros, (size_t)count, "zero points");
     if (s == AQ_OK) s = alloc(&L->d_zero, 256, "zero block");
+    if (s == AQ_OK && d.max_tokens > aq::kFewTokens) {
+        L->sum_groups = (G + 1) / 2 * 2;
+        s = alloc(&L->d_sums, (size_t)d.max_tokens * L->sum_groups * 16, "group sums");
+        // the plan's token counts change only at multiples of 128; a split holds at most 512 tiles
+        size_t need = 0;
+        for (int64_t n = 128; n < d.max_tokens + 128 && n <= 128 * 512; n += 128) {
+            const int64_t t = std::min(n, d.max_tokens);
+            const aq::UsqPlan p = aq::usq_plan(t, d.out_features, L->nchunk);
+            if (p.splits > 1) need = std::max(need, (size_t)p.splits * t * d.out_features * 4);
+        }
+        if (s == AQ_OK && need) s = alloc(&L->d_part, need, "partial sums");
+    }
     uint8_t* tmp = nullptr;
     if (s == AQ_OK) s = alloc(&tmp, std::max(code_bytes, group_count * 2), "staging buffer");
     if (s != AQ_OK) return s;
@@ -373,7 +687,7 @@ aq_status check_call(const aq_usq* L, const void* in, const void* out, int64_t n
 aq::UsqArgs make_args(const aq_usq* L, const void* X, void* Y, int64_t n) {
     return aq::UsqArgs{L->d_codes, L->d_scales, L->d_zeros, static_cast<const uint16_t*>(X), Y, L->desc.y_dtype,
                        (int)n, L->desc.in_features, L->desc.out_features, L->nchunk, L->groups,
-                       std::max(1, L->desc.group / 128)};
+                       std::max(1, L->desc.group / 128), L->d_zero, L->d_sums, L->sum_groups, nullptr, 0};
 }
 
 }  // namespace
@@ -430,8 +744,8 @@ aq_status aq_usq_forward(aq_usq* L, const void* X, void* Y, int64_t n, void* str
     if (s != AQ_OK) return s;
     const aq::UsqArgs a = make_args(L, X, Y, n);
     const auto st = static_cast<hipStream_t>(stream);
-    const hipError_t e = L->desc.dtype == AQ_F16 ? aq::launch_usq_forward<AQ_F16>(a, L->desc.group, st)
-                                                 : aq::launch_usq_forward<AQ_BF16>(a, L->desc.group, st);
+    const hipError_t e = L->desc.dtype == AQ_F16 ? aq::launch_usq_forward<AQ_F16>(a, L->desc.group, L->d_part, st)
+                                                 : aq::launch_usq_forward<AQ_BF16>(a, L->desc.group, L->d_part, st);
     return e == hipSuccess ? AQ_OK : api_hip_fail(e, "forward launch");
 }
 
