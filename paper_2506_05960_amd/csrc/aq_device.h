@@ -45,6 +45,13 @@ __device__ __forceinline__ void lds_dma16(const uint8_t* src, uint8_t* dst_wave_
                                      (__attribute__((address_space(3))) void*)dst_wave_base, 16, 0, 0);
 }
 
+// The same from a buffer, at byte offset `off` (a lane's) + `soff` (uniform).
+__device__ __forceinline__ void lds_dma16(__amdgpu_buffer_rsrc_t src, uint32_t off, uint32_t soff,
+                                          uint8_t* dst_wave_base) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst_wave_base, 16, (int)off,
+                                             (int)soff, 0, 0);
+}
+
 // s_waitcnt with vmcnt <= n (n < 64), expcnt and lgkmcnt unrestricted (gfx9 encoding)
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {

@@ -26,7 +26,7 @@ namespace aq {
 struct GemmOperands {
     const uint16_t* A;
     const uint16_t* B;
-    int64_t lda, ldb;      // row pitches in elements (multiples of 8)
+    int64_t lda, ldb;      // row pitches in elements (multiples of 8, at most kMaxPitch)
     int M, N, K;           // K a multiple of 8
     const uint8_t* zero;   // 16 zero bytes
     int tiles_m, tiles_n;
@@ -34,6 +34,8 @@ struct GemmOperands {
 };
 
 constexpr int kGemmChunk = 64;
+// a tile's 255 rows stay within 32-bit byte offsets
+constexpr int64_t kMaxPitch = 1 << 22;
 
 template <int DT>
 __device__ __forceinline__ floatx16 mfma_gemm(const u32x4& a, const u32x4& b, const floatx16& c) {
@@ -56,7 +58,7 @@ struct GemmTile {
     static constexpr int kLds = 2 * kStage;
     static constexpr int LA = BM * 8 / kThreads, LB = BN * 8 / kThreads;   // 16-byte loads a thread and chunk
     static_assert(BM * 8 % kThreads == 0 && BN * 8 % kThreads == 0, "whole loads");
-    static_assert(kThreads % 64 == 0 && kThreads / 8 % 8 == 0, "one slot permutation a thread");
+    static_assert(kThreads % 64 == 0 && kThreads / 8 % 16 == 0, "one slot permutation a thread");
 };
 
 // Tile of this workgroup: consecutive workgroups go to different XCDs, so each
@@ -84,28 +86,39 @@ __device__ __forceinline__ void gemm_mainloop(const GemmOperands& g, int m0, int
     const int wm = wave / WN, wn = wave - wm * WN;
     const int l32 = lane & 31, hi = lane >> 5;
 
+    // One load a thread: 16 bytes of row r0 + j * rows; whole chunks go through buffer loads (the row's
+    // offset in a register, the chunk's in a scalar: no address arithmetic), the last part of a chunk
+    // through addresses that point past K's end at the zero block.
+    constexpr int kRows = T::kThreads / 8;
     const int r0 = tid >> 3;
-    const int slot = (tid & 7) ^ (r0 & 7);
-    const uint16_t* pa[T::LA];
-    const uint16_t* pb[T::LB];
+    const int slot = (tid & 7) ^ ((r0 >> 1) & 7);
+    const uint16_t* ta = g.A + (int64_t)m0 * g.lda;
+    const uint16_t* tb = g.B + (int64_t)n0 * g.ldb;
+    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(ta, 0xFFFFFFFFu), rb = buffer_rsrc(tb, 0xFFFFFFFFu);
+    const int ma = min(T::BM, g.M - m0) - 1, mb = min(T::BN, g.N - n0) - 1;
+    uint32_t oa[T::LA], ob[T::LB];
 #pragma unroll
-    for (int j = 0; j < T::LA; ++j)
-        pa[j] = g.A + (int64_t)min(m0 + r0 + j * (T::kThreads / 8), g.M - 1) * g.lda + 8 * slot;
+    for (int j = 0; j < T::LA; ++j) oa[j] = (uint32_t)(min(r0 + j * kRows, ma) * (int)g.lda + 8 * slot) * 2u;
 #pragma unroll
-    for (int j = 0; j < T::LB; ++j)
-        pb[j] = g.B + (int64_t)min(n0 + r0 + j * (T::kThreads / 8), g.N - 1) * g.ldb + 8 * slot;
-
-    auto issue = [&](int chunk, uint8_t* st) {
+    for (int j = 0; j < T::LB; ++j) ob[j] = (uint32_t)(min(r0 + j * kRows, mb) * (int)g.ldb + 8 * slot) * 2u;
+    auto issue_whole = [&](int i, int chunk, uint8_t* st) {      // load i of LA + LB of a whole chunk
+        const uint32_t off = i < T::LA ? oa[i < T::LA ? i : 0] : ob[i < T::LA ? 0 : i - T::LA];
+        lds_dma16(i < T::LA ? ra : rb, off, (uint32_t)chunk * (kGemmChunk * 2u), st + (i * T::kThreads + wave * 64) * 16);
+    };
+    auto issue_one = [&](int i, int chunk, uint8_t* st) {
+        uint8_t* dst = st + (i * T::kThreads + wave * 64) * 16;
         const int k0 = chunk * kGemmChunk;
-        const bool in = k0 + 8 * slot < g.K;
+        const uint32_t off = i < T::LA ? oa[i < T::LA ? i : 0] : ob[i < T::LA ? 0 : i - T::LA];
+        if (k0 + kGemmChunk <= g.K) {
+            lds_dma16(i < T::LA ? ra : rb, off, (uint32_t)k0 * 2u, dst);
+        } else {
+            const uint8_t* p = reinterpret_cast<const uint8_t*>((i < T::LA ? ta : tb) + k0) + off;
+            lds_dma16(k0 + 8 * slot < g.K ? p : g.zero, dst);
+        }
+    };
+    auto issue = [&](int chunk, uint8_t* st) {
 #pragma unroll
-        for (int j = 0; j < T::LA; ++j)
-            lds_dma16(in ? reinterpret_cast<const uint8_t*>(pa[j] + k0) : g.zero,
-                      st + (j * T::kThreads + wave * 64) * 16);
-#pragma unroll
-        for (int j = 0; j < T::LB; ++j)
-            lds_dma16(in ? reinterpret_cast<const uint8_t*>(pb[j] + k0) : g.zero,
-                      st + T::BM * 128 + (j * T::kThreads + wave * 64) * 16);
+        for (int i = 0; i < T::LA + T::LB; ++i) issue_one(i, chunk, st);
     };
 #pragma unroll
     for (int a = 0; a < AM; ++a)
@@ -116,29 +129,59 @@ __device__ __forceinline__ void gemm_mainloop(const GemmOperands& g, int m0, int
 
     const uint32_t arow = (uint32_t)(wm * AM * 32 + l32) * 128u;
     const uint32_t brow = (uint32_t)(T::BM + wn * AN * 32 + l32) * 128u;
-    auto compute = [&](const uint8_t* st) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const uint32_t off = (uint32_t)(((2 * s + hi) ^ (l32 & 7)) * 16);
-            u32x4 af[AM], bf[AN];
-#pragma unroll
-            for (int b = 0; b < AN; ++b) bf[b] = *reinterpret_cast<const u32x4*>(st + brow + b * 4096 + off);
-#pragma unroll
-            for (int a = 0; a < AM; ++a) af[a] = *reinterpret_cast<const u32x4*>(st + arow + a * 4096 + off);
-#pragma unroll
-            for (int a = 0; a < AM; ++a)
-#pragma unroll
-                for (int b = 0; b < AN; ++b) acc[a][b] = mfma_gemm<DT>(af[a], bf[b], acc[a][b]);
-        }
+    // operand i of AN + AM of step s (16 values of K) of a stage
+    auto operand = [&](const uint8_t* st, int s, int i) {
+        const uint32_t off = (uint32_t)(((2 * s + hi) ^ ((l32 >> 1) & 7)) * 16);
+        return *reinterpret_cast<const u32x4*>(st + (i < AN ? brow + i * 4096 : arow + (i - AN) * 4096) + off);
     };
     if (c_beg >= c_end) return;
+    // Step s + 1's operands are read between step s's products.  A chunk's last step multiplies after the
+    // barrier that hands over its stage, so that the next chunk's first operands and the loads of the
+    // chunk after it are on their way under those products.
+    u32x4 f[2][AN + AM];
+    constexpr int kOps = AN + AM, kProducts = AM * AN, kLoads = T::LA + T::LB;
     issue(c_beg, lds);
-    for (int c = c_beg; c < c_end; ++c) {
-        const int p = (c - c_beg) & 1;
-        wait_vmcnt<0>();      // this wave's part of chunk c landed
-        lds_barrier();        // everyone's; and every wave is done with the other stage
-        if (c + 1 < c_end) issue(c + 1, lds + (p ^ 1) * T::kStage);
-        compute(lds + p * T::kStage);
+    wait_vmcnt<0>();
+    lds_barrier();
+    if (c_beg + 1 < c_end) issue(c_beg + 1, lds + T::kStage);
+#pragma unroll
+    for (int i = 0; i < kOps; ++i) f[0][i] = operand(lds, 0, i);
+    // the reads are early in a step, so that the wait for them finds them done
+    auto step = [&](const uint8_t* from, int s, auto&& load) {
+#pragma unroll
+        for (int i = 0; i < kProducts; ++i) {
+#pragma unroll
+            for (int q = 2 * i; q < min(2 * i + 2, kOps); ++q) f[(s + 1) & 1][q] = operand(from, (s + 1) & 3, q);
+            load(i);
+            acc[i / AN][i % AN] = mfma_gemm<DT>(f[s & 1][AN + i / AN], f[s & 1][i % AN], acc[i / AN][i % AN]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto none = [](int) {};
+    int c = c_beg;
+    for (; c + 2 < c_end && (c + 3) * kGemmChunk <= g.K; ++c) {       // the chunk loaded is a whole one
+        uint8_t* st = lds + ((c - c_beg) & 1) * T::kStage;
+        uint8_t* next = lds + ((c + 1 - c_beg) & 1) * T::kStage;
+#pragma unroll
+        for (int s = 0; s < 3; ++s) step(st, s, none);
+        wait_vmcnt<0>();      // this wave's part of chunk c + 1 landed
+        lds_barrier();        // everyone's; and every wave has read all of chunk c
+        step(next, 3, [&](int i) {
+#pragma unroll
+            for (int q = i * kLoads / kProducts; q < (i + 1) * kLoads / kProducts; ++q) issue_whole(q, c + 2, st);
+        });
+    }
+    for (; c < c_end; ++c) {                                         // the last two or three
+        uint8_t* st = lds + ((c - c_beg) & 1) * T::kStage;
+        uint8_t* next = lds + ((c + 1 - c_beg) & 1) * T::kStage;
+#pragma unroll
+        for (int s = 0; s < 3; ++s) step(st, s, none);
+        if (c + 1 < c_end) {
+            wait_vmcnt<0>();
+            lds_barrier();
+            if (c + 2 < c_end) issue(c + 2, st);
+        }
+        step(next, 3, none);  // (the last chunk's reads of the other stage are not used)
     }
 }
 

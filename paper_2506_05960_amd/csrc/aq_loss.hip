@@ -578,7 +578,8 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
     if (desc->features && desc->dtype == AQ_F32)
         return api_fail(AQ_ERR_UNSUPPORTED, "the cross entropy takes fp16 or bf16 inputs and head weights");
     if (desc->features % 8 != 0) return api_fail(AQ_ERR_UNSUPPORTED, "features must be a multiple of 8");
-    if (desc->features > (1 << 20)) return api_fail(AQ_ERR_UNSUPPORTED, "features above 2^20");
+    if (desc->features > aq::kMaxPitch || (desc->features && desc->max_tokens > aq::kMaxPitch))
+        return api_fail(AQ_ERR_UNSUPPORTED, "features, or max_tokens of a cross entropy, above 2^22");
     int ndev = 0;
     hipError_t e = hipGetDeviceCount(&ndev);
     if (e != hipSuccess || ndev < 1) return api_fail(AQ_ERR_DEVICE, "no HIP device available");
@@ -592,8 +593,9 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
     }
     if (desc->features) {
         // a piece's gradient and its transposed head rows take at most 128 MiB each
-        const int64_t most = (int64_t(64) << 20) / std::max<int64_t>(desc->max_tokens, desc->features);
-        const int64_t pieces = (desc->vocab + std::max<int64_t>(most, 256) - 1) / std::max<int64_t>(most, 256);
+        const int64_t most = std::min(aq::kMaxPitch / 2, std::max<int64_t>(256, (int64_t(64) << 20) / std::max<int64_t>(
+                                                                              desc->max_tokens, desc->features)));
+        const int64_t pieces = (desc->vocab + most - 1) / most;
         L->piece = (int)(((desc->vocab + pieces - 1) / pieces + 255) / 256 * 256);
         const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 255) / 256;
         aq_status s = alloc(&L->d_zero, 256, "zero block");

@@ -269,8 +269,8 @@ __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
 //    three, six of the eight values a lane holds for one group.
 // SG: steps of 16 inputs a group within a chunk.
 template <int DT, int SG, int AM, int AN>
-__global__ void __launch_bounds__(256, AM == 4 ? 1 : 2) usq_gemm_kernel(UsqArgs a) {
-    constexpr int BM = 64 * AM, BN = 64 * AN, AP = AM < 2 ? 1 : 2;
+__global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
+    constexpr int BM = 64 * AM, BN = 64 * AN;
     constexpr int STAGE = BM * 256, LOADS = BM * 16 / 256;
     extern __shared__ __attribute__((aligned(16))) uint8_t usq_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(256, AM == 4 ? 1 : 2) usq_gemm_kernel(UsqArgs 
     const int c_beg = z * a.cps, c_end = min(a.nchunk, c_beg + a.cps);
 
     // ---- staging of the tokens ----
-    const int r0 = tid >> 4, slot = (tid & 15) ^ (r0 & 7);
+    const int r0 = tid >> 4, slot = (tid & 15) ^ (r0 & 15);
     const uint16_t* px[LOADS];
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) px[j] = a.X + (int64_t)min(m0 + r0 + 16 * j, a.n - 1) * a.K + 8 * slot;
@@ -377,12 +377,12 @@ __global__ void __launch_bounds__(256, AM == 4 ? 1 : 2) usq_gemm_kernel(UsqArgs 
         const uint8_t* st = usq_lds + ((c - c_beg) & 1) * STAGE;
         wait_vmcnt<0>();
         lds_barrier();
-        u32x4 q[AN][8];
+        u32x4 w[AN][2];
         float s32[AN][GPC];
 #pragma unroll
         for (int b = 0; b < AN; ++b) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) q[b][u] = widen_codes<DT>(wc[b][u & 1][u >> 1]);
+            w[b][0] = wc[b][0];
+            w[b][1] = wc[b][1];
 #pragma unroll
             for (int g = 0; g < GPC; ++g) s32[b][g] = widen16<DT>(sc[b][g]);
         }
@@ -390,40 +390,44 @@ __global__ void __launch_bounds__(256, AM == 4 ? 1 : 2) usq_gemm_kernel(UsqArgs 
             issue(c + 1, usq_lds + ((c + 1 - c_beg) & 1) * STAGE);
             load_weights(c + 1);
         }
+        // step u's operands: tokens from LDS, weights widened
+        auto operands = [&](int u, u32x4 (&xf)[AM], u32x4 (&q)[AN]) {
 #pragma unroll
-        for (int x0 = 0; x0 < AM; x0 += AP)
+            for (int x = 0; x < AM; ++x)
+                xf[x] = *reinterpret_cast<const u32x4*>(st + arow + x * 8192 + (((2 * u + hi) ^ (l32 & 15)) * 16));
 #pragma unroll
-            for (int g = 0; g < GPC; ++g) {
-                floatx16 d[AP][AN];
+            for (int b = 0; b < AN; ++b) q[b] = widen_codes<DT>(w[b][u & 1][u >> 1]);
+        };
+        u32x4 xf[2][AM], q[2][AN];
+        operands(0, xf[0], q[0]);
 #pragma unroll
-                for (int u = g * SG; u < (g + 1) * SG; ++u) {
-                    u32x4 xf[AP];
+        for (int g = 0; g < GPC; ++g) {
+            floatx16 d[AM][AN];
 #pragma unroll
-                    for (int x = 0; x < AP; ++x)
-                        xf[x] = *reinterpret_cast<const u32x4*>(st + arow + (x0 + x) * 8192 +
-                                                                (((2 * u + hi) ^ (l32 & 7)) * 16));
+            for (int u = g * SG; u < (g + 1) * SG; ++u) {
+                if (u + 1 < 8) operands(u + 1, xf[(u + 1) & 1], q[(u + 1) & 1]);
 #pragma unroll
-                    for (int x = 0; x < AP; ++x)
+                for (int x = 0; x < AM; ++x)
 #pragma unroll
-                        for (int b = 0; b < AN; ++b) {
-                            if (u == g * SG) {
-                                floatx16 zero;
+                    for (int b = 0; b < AN; ++b) {
+                        if (u == g * SG) {
+                            floatx16 zero;
 #pragma unroll
-                                for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
-                                d[x][b] = mfma_gemm<DT>(xf[x], q[b][u], zero);
-                            } else {
-                                d[x][b] = mfma_gemm<DT>(xf[x], q[b][u], d[x][b]);
-                            }
+                            for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+                            d[x][b] = mfma_gemm<DT>(xf[u & 1][x], q[u & 1][b], zero);
+                        } else {
+                            d[x][b] = mfma_gemm<DT>(xf[u & 1][x], q[u & 1][b], d[x][b]);
                         }
-                }
-#pragma unroll
-                for (int x = 0; x < AP; ++x)
-#pragma unroll
-                    for (int b = 0; b < AN; ++b)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            acc[x0 + x][b][r] = __builtin_fmaf(s32[b][g], d[x][b][r], acc[x0 + x][b][r]);
+                    }
             }
+#pragma unroll
+            for (int x = 0; x < AM; ++x)
+#pragma unroll
+                for (int b = 0; b < AN; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        acc[x][b][r] = __builtin_fmaf(s32[b][g], d[x][b][r], acc[x][b][r]);
+        }
     }
 
     float* part = a.part ? a.part + (int64_t)z * a.n * a.C_out : nullptr;
@@ -462,12 +466,11 @@ struct UsqPlan {
 UsqPlan usq_plan(int64_t n, int C_out, int nchunk) {
     UsqPlan p;
     const int64_t tn = (C_out + 127) / 128;
-    p.am = (n + 255) / 256 * tn >= 256 ? 4 : 2;
+    p.am = 2;
     const int64_t tiles = (n + 64 * p.am - 1) / (64 * p.am) * tn;
     p.tiles = (int)tiles;
     const int most = std::max(1, nchunk / 4);
     int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / tiles));
-    if (p.am == 4) splits = 1;
     p.cps = (nchunk + splits - 1) / splits;
     p.splits = (nchunk + p.cps - 1) / p.cps;
     return p;
@@ -492,8 +495,7 @@ hipError_t launch_many(UsqArgs a, int group, float* part, hipStream_t st) {
     if (e != hipSuccess) return e;
     a.cps = p.cps;
     a.part = p.splits > 1 ? part : nullptr;
-    e = p.am == 4 ? launch_usq_gemm<DT, SG, 4, 2>(a, p.tiles * p.splits, st)
-                  : launch_usq_gemm<DT, SG, 2, 2>(a, p.tiles * p.splits, st);
+    e = launch_usq_gemm<DT, SG, 2, 2>(a, p.tiles * p.splits, st);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t count = (int64_t)a.n * a.C_out;
     usq_join_kernel<<<(unsigned)std::min<int64_t>((count + 255) / 256, 4096), 256, 0, st>>>(part, p.splits, count, a.Y,
@@ -710,8 +712,8 @@ aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* 
     if (d.in_features % 8 != 0) return api_fail(AQ_ERR_UNSUPPORTED, "in_features must be a multiple of 8");
     if (d.group != 32 && d.group != 64 && d.group % 128 != 0)
         return api_fail(AQ_ERR_UNSUPPORTED, "group must be 32, 64 or a multiple of 128");
-    if (d.in_features > (1 << 24) || d.out_features > (1 << 24) || d.max_tokens > (1 << 24))
-        return api_fail(AQ_ERR_UNSUPPORTED, "sizes above 2^24");
+    if (d.in_features > aq::kMaxPitch || d.out_features > aq::kMaxPitch || d.max_tokens > (1 << 24))
+        return api_fail(AQ_ERR_UNSUPPORTED, "features above 2^22 or max_tokens above 2^24");
     if (zeros) {
         const int64_t count = (int64_t)d.out_features * ((d.in_features + (int64_t)d.group - 1) / d.group);
         for (int64_t i = 0; i < count; ++i)
