@@ -228,7 +228,7 @@ hipError_t launch_few(const UsqArgs& a, hipStream_t st) {
 // ---- many tokens ----
 
 // Group sums of the inputs, S[t][j], as three bf16 pieces that add up to the
-// fp32 sum: [n][groups rounded up to 2][8] = {h, m, l, h, m, l, 0, 0}.
+// fp32 sum: [group][n][8] = {h, m, l, h, m, l, 0, 0}.
 template <int DT>
 __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
     // eight lanes a group, 16-byte loads
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
     const float r1 = s - bf16_to_f32((uint16_t)h);
     const uint32_t m = f32_to_bf16(r1);
     const uint32_t l = f32_to_bf16(r1 - bf16_to_f32((uint16_t)m));
-    reinterpret_cast<u32x4*>(a.sums)[id] = u32x4{h | m << 16, l | h << 16, m | l << 16, 0u};
+    reinterpret_cast<u32x4*>(a.sums)[(int64_t)j * a.n + t] = u32x4{h | m << 16, l | h << 16, m | l << 16, 0u};
 }
 
 // A 2 x 2 grid of waves on a (64 AM) x (64 AN) tile of tokens x output rows;
@@ -268,13 +268,14 @@ __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
 //    groups, of s z in two bf16 pieces (15 bits at most, exact) and the sums in
 //    three, six of the eight values a lane holds for one group.
 // SG: steps of 16 inputs a group within a chunk.
-template <int DT, int SG, int AM, int AN>
+template <int DT, int SG, int WM, int WN, int AM, int AN>
 __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
-    constexpr int BM = 64 * AM, BN = 64 * AN;
+    constexpr int BM = 32 * WM * AM, BN = 32 * WN * AN;
+    static_assert(WM * WN == 4, "four waves");
     constexpr int STAGE = BM * 256, LOADS = BM * 16 / 256;
     extern __shared__ __attribute__((aligned(16))) uint8_t usq_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave & 1, wn = wave >> 1, l32 = lane & 31, hi = lane >> 5;
+    const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
     // XCD-aware order: each XCD takes a contiguous run, token tiles fastest in bands of eight
     const int tiles_m = (a.n + BM - 1) / BM, tiles_n = (a.C_out + BN - 1) / BN;
     int tm, tn, z;
@@ -294,15 +295,26 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
 
     // ---- staging of the tokens ----
     const int r0 = tid >> 4, slot = (tid & 15) ^ (r0 & 15);
-    const uint16_t* px[LOADS];
+    // a whole chunk through buffer loads (the row's offset in a register, the chunk's in a scalar), the last
+    // part of a chunk through addresses that point past K's end at the zero block
+    const uint16_t* tx = a.X + (int64_t)m0 * a.K;
+    const __amdgpu_buffer_rsrc_t rx = buffer_rsrc(tx, 0xFFFFFFFFu);
+    const int mx = min(BM, a.n - m0) - 1;
+    uint32_t ox[LOADS];
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) px[j] = a.X + (int64_t)min(m0 + r0 + 16 * j, a.n - 1) * a.K + 8 * slot;
+    for (int j = 0; j < LOADS; ++j) ox[j] = (uint32_t)(min(r0 + 16 * j, mx) * a.K + 8 * slot) * 2u;
     auto issue = [&](int chunk, uint8_t* st) {
         const int k0 = chunk * 128;
-        const bool in = k0 + 8 * slot < a.K;
+        if (k0 + 128 <= a.K) {
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j)
-            lds_dma16(in ? reinterpret_cast<const uint8_t*>(px[j] + k0) : a.zero, st + (j * 256 + wave * 64) * 16);
+            for (int j = 0; j < LOADS; ++j) lds_dma16(rx, ox[j], (uint32_t)k0 * 2u, st + (j * 256 + wave * 64) * 16);
+        } else {
+            const bool in = k0 + 8 * slot < a.K;
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j)
+                lds_dma16(in ? reinterpret_cast<const uint8_t*>(tx + k0) + ox[j] : a.zero,
+                          st + (j * 256 + wave * 64) * 16);
+        }
     };
 
     // ---- weights: this lane's column of each block, two 16-byte loads a chunk ----
@@ -341,6 +353,17 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
 
     issue(c_beg, usq_lds);
     load_weights(c_beg);
+    u32x4 w[AN][2];              // the chunk's codes and scales, while the next one's are loaded
+    float s32[AN][GPC];
+    auto take_weights = [&]() {
+#pragma unroll
+        for (int b = 0; b < AN; ++b) {
+            w[b][0] = wc[b][0];
+            w[b][1] = wc[b][1];
+#pragma unroll
+            for (int g = 0; g < GPC; ++g) s32[b][g] = widen16<DT>(sc[b][g]);
+        }
+    };
     // ---- zero points of the groups that begin in this split's chunks ----
     {
         const int j_beg = GPC == 1 ? (c_beg + a.per - 1) / a.per : c_beg * GPC;
@@ -348,8 +371,7 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
         const u32x4* ps[AM];
 #pragma unroll
         for (int x = 0; x < AM; ++x)
-            ps[x] = reinterpret_cast<const u32x4*>(a.sums) +
-                    (int64_t)min(m0 + (wm * AM + x) * 32 + l32, a.n - 1) * a.sum_groups;
+            ps[x] = reinterpret_cast<const u32x4*>(a.sums) + min(m0 + (wm * AM + x) * 32 + l32, a.n - 1);
 #pragma unroll 2
         for (int j0 = j_beg; j0 < j_end; j0 += 2) {
             const int j = min(j0 + hi, j_end - 1);
@@ -357,7 +379,7 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
             u32x4 fs[AM];
 #pragma unroll
             for (int x = 0; x < AM; ++x) {
-                fs[x] = ps[x][min(j, a.sum_groups - 1)];
+                fs[x] = ps[x][(int64_t)min(j, a.sum_groups - 1) * a.n];
                 if (!live) fs[x] = u32x4{0, 0, 0, 0};
             }
 #pragma unroll
@@ -372,63 +394,89 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
         }
     }
 
+    // ---- products ----
+    // Step u + 1's operands are read and widened between step u's products; a chunk's last step multiplies
+    // behind the barrier that hands its stage over; and a group's sum is scaled into the running sum
+    // between the first products of the next group, block by block.
     const uint32_t arow = (uint32_t)(wm * AM * 32 + l32) * 256u;
+    u32x4 xf[2][AM], q[2][AN];
+    auto operand = [&](const uint8_t* st, int u, int i) {
+        if (i < AM)
+            xf[u & 1][i] = *reinterpret_cast<const u32x4*>(st + arow + i * 8192 + (((2 * u + hi) ^ (l32 & 15)) * 16));
+        else q[u & 1][i - AM] = widen_codes<DT>(w[i - AM][u & 1][u >> 1]);
+    };
+    floatx16 d[AM][AN];
+    float sprev[AN];
+#pragma unroll
+    for (int b = 0; b < AN; ++b) sprev[b] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < AM; ++x)
+#pragma unroll
+        for (int b = 0; b < AN; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) d[x][b][r] = 0.0f;
+    auto scale = [&](int x, int b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[x][b][r] = __builtin_fmaf(sprev[b], d[x][b][r], acc[x][b][r]);
+    };
+    wait_vmcnt<0>();
+    lds_barrier();
+    take_weights();
+    if (c_beg + 1 < c_end) {
+        issue(c_beg + 1, usq_lds + STAGE);
+        load_weights(c_beg + 1);
+    }
+#pragma unroll
+    for (int i = 0; i < AM + AN; ++i) operand(usq_lds, 0, i);
+    constexpr int kOps = AM + AN, kProducts = AM * AN;
     for (int c = c_beg; c < c_end; ++c) {
-        const uint8_t* st = usq_lds + ((c - c_beg) & 1) * STAGE;
-        wait_vmcnt<0>();
-        lds_barrier();
-        u32x4 w[AN][2];
-        float s32[AN][GPC];
+        uint8_t* st = usq_lds + ((c - c_beg) & 1) * STAGE;
+        const uint8_t* next = usq_lds + ((c + 1 - c_beg) & 1) * STAGE;
+        float snext[AN][GPC];
 #pragma unroll
-        for (int b = 0; b < AN; ++b) {
-            w[b][0] = wc[b][0];
-            w[b][1] = wc[b][1];
+        for (int b = 0; b < AN; ++b)
 #pragma unroll
-            for (int g = 0; g < GPC; ++g) s32[b][g] = widen16<DT>(sc[b][g]);
-        }
-        if (c + 1 < c_end) {
-            issue(c + 1, usq_lds + ((c + 1 - c_beg) & 1) * STAGE);
-            load_weights(c + 1);
-        }
-        // step u's operands: tokens from LDS, weights widened
-        auto operands = [&](int u, u32x4 (&xf)[AM], u32x4 (&q)[AN]) {
+            for (int g = 0; g < GPC; ++g) snext[b][g] = s32[b][g];
 #pragma unroll
-            for (int x = 0; x < AM; ++x)
-                xf[x] = *reinterpret_cast<const u32x4*>(st + arow + x * 8192 + (((2 * u + hi) ^ (l32 & 15)) * 16));
-#pragma unroll
-            for (int b = 0; b < AN; ++b) q[b] = widen_codes<DT>(w[b][u & 1][u >> 1]);
-        };
-        u32x4 xf[2][AM], q[2][AN];
-        operands(0, xf[0], q[0]);
-#pragma unroll
-        for (int g = 0; g < GPC; ++g) {
-            floatx16 d[AM][AN];
-#pragma unroll
-            for (int u = g * SG; u < (g + 1) * SG; ++u) {
-                if (u + 1 < 8) operands(u + 1, xf[(u + 1) & 1], q[(u + 1) & 1]);
-#pragma unroll
-                for (int x = 0; x < AM; ++x)
-#pragma unroll
-                    for (int b = 0; b < AN; ++b) {
-                        if (u == g * SG) {
-                            floatx16 zero;
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
-                            d[x][b] = mfma_gemm<DT>(xf[u & 1][x], q[u & 1][b], zero);
-                        } else {
-                            d[x][b] = mfma_gemm<DT>(xf[u & 1][x], q[u & 1][b], d[x][b]);
-                        }
-                    }
+        for (int u = 0; u < 8; ++u) {
+            if (u == 7 && c + 1 < c_end) {
+                wait_vmcnt<0>();     // this wave's part of chunk c + 1 landed, its codes too
+                lds_barrier();       // everyone's; and every wave has read all of chunk c
+                take_weights();
+                if (c + 2 < c_end) {
+                    issue(c + 2, st);
+                    load_weights(c + 2);
+                }
             }
 #pragma unroll
-            for (int x = 0; x < AM; ++x)
+            for (int i = 0; i < kProducts; ++i) {
+                // (the last chunk's reads of the other stage are not used)
 #pragma unroll
-                for (int b = 0; b < AN; ++b)
+                for (int o = 2 * i; o < (i + 1 == kProducts ? kOps : min(2 * i + 2, kOps)); ++o)
+                    operand(u < 7 ? st : next, (u + 1) & 7, o);
+                const int x = i / AN, b = i % AN;
+                if (u % SG == 0) {
+                    scale(x, b);
+                    asm volatile("" : "+v"(acc[x][b]));      // before the group's sum is overwritten
+                    floatx16 zero;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        acc[x][b][r] = __builtin_fmaf(s32[b][g], d[x][b][r], acc[x][b][r]);
+                    for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+                    d[x][b] = mfma_gemm<DT>(xf[u & 1][x], q[u & 1][b], zero);
+                } else {
+                    d[x][b] = mfma_gemm<DT>(xf[u & 1][x], q[u & 1][b], d[x][b]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (u % SG == 0) {
+#pragma unroll
+                for (int b = 0; b < AN; ++b) sprev[b] = snext[b][u / SG];
+            }
         }
     }
+#pragma unroll
+    for (int x = 0; x < AM; ++x)
+#pragma unroll
+        for (int b = 0; b < AN; ++b) scale(x, b);
 
     float* part = a.part ? a.part + (int64_t)z * a.n * a.C_out : nullptr;
 #pragma unroll
@@ -476,10 +524,10 @@ UsqPlan usq_plan(int64_t n, int C_out, int nchunk) {
     return p;
 }
 
-template <int DT, int SG, int AM, int AN>
+template <int DT, int SG, int WM, int WN, int AM, int AN>
 hipError_t launch_usq_gemm(const UsqArgs& a, int grid, hipStream_t st) {
-    constexpr size_t lds = 2 * 64 * AM * 256;
-    auto kern = usq_gemm_kernel<DT, SG, AM, AN>;
+    constexpr size_t lds = 2 * 32 * WM * AM * 256;
+    auto kern = usq_gemm_kernel<DT, SG, WM, WN, AM, AN>;
     const hipError_t e = ensure_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;
     kern<<<(unsigned)grid, 256, lds, st>>>(a);
@@ -495,7 +543,7 @@ hipError_t launch_many(UsqArgs a, int group, float* part, hipStream_t st) {
     if (e != hipSuccess) return e;
     a.cps = p.cps;
     a.part = p.splits > 1 ? part : nullptr;
-    e = launch_usq_gemm<DT, SG, 2, 2>(a, p.tiles * p.splits, st);
+    e = launch_usq_gemm<DT, SG, 1, 4, 4, 1>(a, p.tiles * p.splits, st);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t count = (int64_t)a.n * a.C_out;
     usq_join_kernel<<<(unsigned)std::min<int64_t>((count + 255) / 256, 4096), 256, 0, st>>>(part, p.splits, count, a.Y,
@@ -630,7 +678,7 @@ aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t
     if (s == AQ_OK && zeros) s = alloc(&L->d_zeros, (size_t)count, "zero points");
     if (s == AQ_OK) s = alloc(&L->d_zero, 256, "zero block");
     if (s == AQ_OK && d.max_tokens > aq::kFewTokens) {
-        L->sum_groups = (G + 1) / 2 * 2;
+        L->sum_groups = G;
         s = alloc(&L->d_sums, (size_t)d.max_tokens * L->sum_groups * 16, "group sums");
         // the plan's token counts change only at multiples of 128; a split holds at most 512 tiles
         size_t need = 0;
