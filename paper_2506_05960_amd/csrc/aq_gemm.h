@@ -2,6 +2,7 @@
 // A [M][K] and B [N][K] row-major (both with K contiguous), and an epilogue
 // that consumes a workgroup's D tile in registers.
 //
+//  * K may be split over workgroups (each split's D is an fp32 sum of its own).
 //  * A workgroup of WM x WN waves owns a (WM * AM * 32) x (WN * AN * 32) tile;
 //    each wave accumulates AM x AN blocks of v_mfma_f32_32x32x16 (rows from A,
 //    columns from B).
@@ -31,6 +32,7 @@ struct GemmOperands {
     const uint8_t* zero;   // 16 zero bytes
     int tiles_m, tiles_n;
     int rows_fast;         // tiles of a band that share their B rows (see gemm_tile)
+    int cps;               // K chunks a split
 };
 
 constexpr int kGemmChunk = 64;
@@ -64,11 +66,13 @@ struct GemmTile {
 // Tile of this workgroup: consecutive workgroups go to different XCDs, so each
 // XCD takes a contiguous run of tiles; a run walks bands of `rows_fast` tiles
 // along M, column by column, so that its L2 serves both operands.
-__device__ __forceinline__ void gemm_tile(const GemmOperands& g, int& tm, int& tn) {
+__device__ __forceinline__ void gemm_tile(const GemmOperands& g, int& tm, int& tn, int& z) {
     const int nwg = (int)gridDim.x, h = (int)blockIdx.x;
     const int xcd = h & 7, j = h >> 3;
     const int per = nwg >> 3, rem = nwg & 7;
-    const int w = xcd * per + min(xcd, rem) + j;
+    int w = xcd * per + min(xcd, rem) + j;
+    z = w / (g.tiles_m * g.tiles_n);
+    w -= z * g.tiles_m * g.tiles_n;
     const int band = w / (g.rows_fast * g.tiles_n);
     const int m0 = band * g.rows_fast;
     const int rows = min(g.rows_fast, g.tiles_m - m0);
@@ -185,58 +189,153 @@ __device__ __forceinline__ void gemm_mainloop(const GemmOperands& g, int m0, int
     }
 }
 
-// D scaled to 16 bits, with an fp32 running sum over several products:
-// D + sum -> sum, or, the last time, -> out.
-template <int DT, int WM, int WN, int AM, int AN>
+// Where a product's D goes: 16-bit results, or fp32 sums that later products
+// of the same output add to.  With K split over workgroups every split keeps a
+// sum of its own, and split_sum_kernel adds them.
+enum StoreMode {
+    STORE_OUT = 0,         // out = D * scale
+    STORE_SUM = 1,         // sum = D
+    STORE_ADD = 2,         // sum += D
+    STORE_LAST = 3         // out = (sum + D) * scale
+};
+
+template <int DT>
+struct StoreArgs {
+    uint16_t* out;         // [M] rows of pitch ldo
+    float* sum;            // [split][M][N]
+    int64_t ldo;           // at most kMaxPitch, as N is
+    const float* scale;    // null: 1
+};
+
+template <int DT, int MODE, int WM, int WN, int AM, int AN>
 struct StoreEpilogue {
-    uint16_t* out;         // [M][ldo] the result; null: the sum goes on
-    float* sum;            // [M][lds]
-    int64_t ldo;
-    int first;             // no sum yet
-    const float* scale;    // the result times *scale (null: 1)
-    __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int m0, int n0, int M, int N, uint8_t*) const {
+    StoreArgs<DT> s;
+
+    // Branch-free buffer accesses at offsets from the tile's corner; positions past D's edge get an offset past
+    // the buffer.
+    __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int z, int m0, int n0, int M, int N, uint8_t*) const {
+        constexpr bool kOut = MODE == STORE_OUT || MODE == STORE_LAST, kOld = MODE == STORE_ADD || MODE == STORE_LAST;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
-        const float f = scale ? *scale : 1.0f;
+        const float f = kOut && s.scale ? *s.scale : 1.0f;
+        const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(s.out + (int64_t)m0 * s.ldo + n0, kOutOfRange);
+        const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(s.sum + ((int64_t)z * M + m0) * N + n0, kOutOfRange);
 #pragma unroll
         for (int a = 0; a < AM; ++a)
 #pragma unroll
-            for (int b = 0; b < AN; ++b)
+            for (int r = 0; r < 16; ++r) {
+                const int m = (wm * AM + a) * 32 + gemm_row(r, hi);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int m = m0 + (wm * AM + a) * 32 + gemm_row(r, hi);
-                    const int n = n0 + (wn * AN + b) * 32 + l32;
-                    if (m >= M || n >= N) continue;
-                    const int64_t i = (int64_t)m * ldo + n;
+                for (int b = 0; b < AN; ++b) {
+                    const int n = (wn * AN + b) * 32 + l32;
+                    const bool in = m0 + m < M && n0 + n < N;
+                    const uint32_t os = in ? (uint32_t)(m * N + n) * 4u : kOutOfRange;
                     float v = acc[a][b][r];
-                    if (!first) v += sum[i];
-                    if (out) out[i] = f32_to_tile<DT>(v * f);
-                    else sum[i] = v;
+                    if (kOld) v += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, os, 0, 0));
+                    if (kOut) {
+                        const uint32_t oo = in ? (uint32_t)(m * (int)s.ldo + n) * 2u : kOutOfRange;
+                        __builtin_amdgcn_raw_buffer_store_b16(f32_to_tile<DT>(v * f), ro, oo, 0, 0);
+                    } else {
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rs, os, 0, 0);
+                    }
                 }
+            }
     }
 };
 
 template <int DT, int WM, int WN, int AM, int AN, class Epi>
-__global__ void __launch_bounds__(WM* WN * 64) gemm_kernel(GemmOperands g, Epi epi) {
+__global__ void __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 1 : 2) gemm_kernel(GemmOperands g, Epi epi) {
     using T = GemmTile<WM, WN, AM, AN>;
     extern __shared__ __attribute__((aligned(16))) uint8_t gemm_lds[];
-    int tm, tn;
-    gemm_tile(g, tm, tn);
+    int tm, tn, z;
+    gemm_tile(g, tm, tn, z);
+    const int chunks = (g.K + kGemmChunk - 1) / kGemmChunk;
     floatx16 acc[AM][AN];
-    gemm_mainloop<DT, WM, WN, AM, AN>(g, tm * T::BM, tn * T::BN, 0, (g.K + kGemmChunk - 1) / kGemmChunk, gemm_lds, acc);
-    epi(acc, tm, tm * T::BM, tn * T::BN, g.M, g.N, gemm_lds);
+    gemm_mainloop<DT, WM, WN, AM, AN>(g, tm * T::BM, tn * T::BN, z * g.cps, min(chunks, (z + 1) * g.cps), gemm_lds, acc);
+    epi(acc, tm, z, tm * T::BM, tn * T::BN, g.M, g.N, gemm_lds);
+}
+
+// Tile and K split of one product.
+struct GemmPlan {
+    bool big;              // 256 x 256 tiles of eight waves, else 128 x 128 of four
+    int splits, cps;       // splits (every one owns a chunk), chunks a split
+};
+
+// Shortest by a model of the calls: rounds of 256 big or 512 small tiles (one
+// or two a compute unit), a tile's fixed time and its time a chunk, and the
+// splits' sums.
+inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, bool may_split) {
+    const int chunks = (int)((K + kGemmChunk - 1) / kGemmChunk);
+    GemmPlan best{true, 1, chunks};
+    double best_us = 1e30;
+    for (int big = 1; big >= 0; --big) {
+        const int64_t side = big ? 256 : 128, slots = big ? 256 : 512;
+        const int64_t tiles = (M + side - 1) / side * ((N + side - 1) / side);
+        const double fixed = big ? 6.0 : 4.0, chunk = big ? 1.75 : 1.0;
+        for (int s = 1; s <= (may_split ? std::min(chunks, 64) : 1); ++s) {
+            if (s > 1 && tiles * (s - 1) >= slots) break;
+            const int cps = (chunks + s - 1) / s;
+            if ((chunks + cps - 1) / cps != s) continue;
+            const int64_t rounds = (tiles * s + slots - 1) / slots;
+            const double us = rounds * (fixed + chunk * cps) + (s > 1 ? 4.0 + 8e-6 * M * N * s / 4 : 0.0);
+            if (us < best_us) {
+                best_us = us;
+                best = GemmPlan{big != 0, s, cps};
+            }
+        }
+    }
+    return best;
 }
 
 template <int DT, int WM, int WN, int AM, int AN, class Epi>
-hipError_t launch_gemm(GemmOperands g, const Epi& epi, hipStream_t st) {
+hipError_t launch_gemm(GemmOperands g, const GemmPlan& p, const Epi& epi, hipStream_t st) {
     using T = GemmTile<WM, WN, AM, AN>;
     g.tiles_m = (g.M + T::BM - 1) / T::BM;
     g.tiles_n = (g.N + T::BN - 1) / T::BN;
     g.rows_fast = std::min(8, g.tiles_m);
+    g.cps = p.cps;
     auto kern = gemm_kernel<DT, WM, WN, AM, AN, Epi>;
     const hipError_t e = ensure_dynamic_lds((const void*)kern, T::kLds);
     if (e != hipSuccess) return e;
-    kern<<<(unsigned)((int64_t)g.tiles_m * g.tiles_n), T::kThreads, T::kLds, st>>>(g, epi);
+    kern<<<(unsigned)((int64_t)g.tiles_m * g.tiles_n * p.splits), T::kThreads, T::kLds, st>>>(g, epi);
+    return hipGetLastError();
+}
+
+template <int DT, int MODE>
+hipError_t launch_store_gemm(const GemmOperands& g, const GemmPlan& p, const StoreArgs<DT>& s, hipStream_t st) {
+    return p.big ? launch_gemm<DT, 2, 4, 4, 2>(g, p, StoreEpilogue<DT, MODE, 2, 4, 4, 2>{s}, st)
+                 : launch_gemm<DT, 2, 2, 2, 2>(g, p, StoreEpilogue<DT, MODE, 2, 2, 2, 2>{s}, st);
+}
+
+template <int DT>
+hipError_t launch_store_gemm(const GemmOperands& g, const GemmPlan& p, const StoreArgs<DT>& s, int mode, hipStream_t st) {
+    return mode == STORE_OUT   ? launch_store_gemm<DT, STORE_OUT>(g, p, s, st)
+           : mode == STORE_SUM ? launch_store_gemm<DT, STORE_SUM>(g, p, s, st)
+           : mode == STORE_ADD ? launch_store_gemm<DT, STORE_ADD>(g, p, s, st)
+                               : launch_store_gemm<DT, STORE_LAST>(g, p, s, st);
+}
+
+// out[m][n] = scale * (sum over the splits, in split order), four values a thread (N a multiple of 8).
+template <int DT>
+__global__ void __launch_bounds__(256) split_sum_kernel(const float* sum, int splits, int64_t M, int N, uint16_t* out,
+                                                        int64_t ldo, const float* scale) {
+    const float f = scale ? *scale : 1.0f;
+    const int64_t count = M * N;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)gridDim.x * 1024) {
+        floatx4 v = *reinterpret_cast<const floatx4*>(sum + i);
+        for (int z = 1; z < splits; ++z) v += *reinterpret_cast<const floatx4*>(sum + z * count + i);
+        const int64_t m = i / N;
+        *reinterpret_cast<uint2*>(out + m * ldo + (i - m * N)) =
+            make_uint2(f32_to_tile<DT>(v[0] * f) | (uint32_t)f32_to_tile<DT>(v[1] * f) << 16,
+                       f32_to_tile<DT>(v[2] * f) | (uint32_t)f32_to_tile<DT>(v[3] * f) << 16);
+    }
+}
+
+template <int DT>
+hipError_t launch_split_sum(const float* sum, int splits, int64_t M, int N, uint16_t* out, int64_t ldo,
+                            const float* scale, hipStream_t st) {
+    const int64_t blocks = (M * N + 1023) / 1024;
+    split_sum_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, scale);
     return hipGetLastError();
 }
 

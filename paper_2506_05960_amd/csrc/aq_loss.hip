@@ -16,7 +16,7 @@ struct aq_loss {
     int device;
     int piece;             // cross entropy: vocabulary rows a piece of the gradient covers
     uint8_t* d_zero;       // 256 zero bytes
-    float2* d_part;        // [vocabulary tile][max_tokens] maximum and sum of exponentials
+    float2* d_part;        // [vocabulary tile of 128][max_tokens] maximum and sum of exponentials
     float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then {scale, 1 / scale}
     // gradient workspace, allocated by the first call that needs it
     uint16_t* d_dl;        // [max_tokens][piece] logits' gradient of a piece
@@ -268,25 +268,30 @@ template <int WM, int WN, int AM, int AN>
 struct StatsEpilogue {
     float2* part;          // [tiles_m][n]
     RowState rs;
-    __device__ void operator()(const floatx16 (&acc)[AM][AN], int tm, int m0, int n0, int M, int N, uint8_t* lds) const {
+    __device__ void operator()(const floatx16 (&acc)[AM][AN], int tm, int, int m0, int n0, int M, int N,
+                               uint8_t* lds) const {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
         float2* red = reinterpret_cast<float2*>(lds);            // [WM][BN]
         constexpr int BN = WN * AN * 32;
         __syncthreads();                                         // the last chunk is read
+        const int v0 = m0 + wm * AM * 32 + 4 * hi;               // vocabulary row of register 0
+        const bool edge = m0 + WM * AM * 32 > M;
 #pragma unroll
         for (int b = 0; b < AN; ++b) {
             const int col = wn * AN * 32 + b * 32 + l32;
             const int t = n0 + col;
-            const int64_t target = t < N ? rs.targets[t] : -1;
+            // the target as a row of this lane's first register
+            const int64_t tv = t < N ? rs.targets[t] : -1;
+            const int target = tv >= 0 && tv < M ? (int)tv - v0 : -1;
             float m = -INFINITY;
 #pragma unroll
             for (int a = 0; a < AM; ++a)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int v = m0 + (wm * AM + a) * 32 + gemm_row(r, hi);
-                    if (v < M) m = fmaxf(m, acc[a][b][r]);
-                    if (v < M && v == target) rs.zt[t] = acc[a][b][r];
+                    const int v = a * 32 + gemm_row(r, 0);
+                    if (!edge || v0 + v < M) m = fmaxf(m, acc[a][b][r]);
+                    if (v == target) rs.zt[t] = acc[a][b][r];
                 }
             const float bm = m == -INFINITY ? 0.0f : m;
             float s = 0.0f;
@@ -294,8 +299,8 @@ struct StatsEpilogue {
             for (int a = 0; a < AM; ++a)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int v = m0 + (wm * AM + a) * 32 + gemm_row(r, hi);
-                    if (v < M) s += exp2_fast((acc[a][b][r] - bm) * kLog2e);
+                    const float e = exp2_fast((acc[a][b][r] - bm) * kLog2e);
+                    if (!edge || v0 + a * 32 + gemm_row(r, 0) < M) s += e;
                 }
             merge(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32), kLog2e);
             if (hi == 0) red[wm * BN + col] = make_float2(m, s);
@@ -322,14 +327,15 @@ struct GradEpilogue {
     int piece, np;         // pitches
     int64_t v0;            // first vocabulary row of the piece
     RowState rs;
-    __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int m0, int n0, int M, int N, uint8_t*) const {
+    __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int, int m0, int n0, int M, int N, uint8_t*) const {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
         const float scale = rs.scale[0];
 #pragma unroll
         for (int b = 0; b < AN; ++b) {
             const int t = n0 + wn * AN * 32 + b * 32 + l32;
-            const int64_t target = t < N ? rs.targets[t] - v0 : -1;
+            const int64_t tv = t < N ? rs.targets[t] - v0 : -1;
+            const int target = tv >= 0 && tv < M ? (int)tv : -1;
             const float top = t < N ? rs.top[t] : 0.0f, ls = t < N ? rs.ls[t] : 0.0f;
             const float w = t < N ? rs.w[t] * scale : 0.0f;
 #pragma unroll
@@ -356,22 +362,23 @@ struct GradEpilogue {
     }
 };
 
-// Maximum, sum, loss and row weight of every token from its tiles' parts.
+// Maximum, sum, loss and row weight of every token from its tiles' parts:
+// sixteen tokens a workgroup, sixteen threads a token.
 __global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* part, int tiles, int n, int64_t V) {
-    __shared__ float2 red[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t = blockIdx.x * 64 + lane;
+    __shared__ float2 red[16][16];
+    const int tok = threadIdx.x & 15, p = threadIdx.x >> 4;
+    const int t = blockIdx.x * 16 + tok;
     float m = -INFINITY, s = 0.0f;
     if (t < n)
-        for (int i = wave; i < tiles; i += 4) {
+        for (int i = p; i < tiles; i += 16) {
             const float2 v = part[(int64_t)i * n + t];
             merge(m, s, v.x, v.y, kLog2e);
         }
-    red[wave][lane] = make_float2(m, s);
+    red[p][tok] = make_float2(m, s);
     __syncthreads();
-    if (wave != 0 || t >= n) return;
+    if (p != 0 || t >= n) return;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) merge(m, s, red[w][lane].x, red[w][lane].y, kLog2e);
+    for (int w = 1; w < 16; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
     const int64_t target = rs.targets[t];
     float ls = __builtin_amdgcn_logf(s);
     float w = rs.dloss ? rs.dloss[t] : 1.0f;
@@ -393,56 +400,73 @@ __global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* pa
 // relative precision whatever the weights' size, and the target's entry, (p - 1) times the weight and often the
 // largest of its row, lies where the type's steps are finest relative to it (equal weights: half the error of the
 // worst factor).
-__global__ void __launch_bounds__(1024) scale_kernel(const float* w, int n, float* scale) {
-    __shared__ float red[16];
+__device__ __forceinline__ float row_weight(const RowState& rs, int64_t t) {
+    return rs.targets[t] < 0 ? 0.0f : rs.dloss ? rs.dloss[t] : 1.0f;
+}
+
+__device__ __forceinline__ void find_scale(const RowState& rs, int n) {
+    __shared__ float red[4];
     float m = 0.0f;
-    for (int i = threadIdx.x; i < n; i += 1024) m = fmaxf(m, fabsf(w[i]));
+    for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, fabsf(row_weight(rs, i)));
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int i = 1; i < 16; ++i) m = fmaxf(m, red[i]);
+    for (int i = 1; i < 4; ++i) m = fmaxf(m, red[i]);
     // (the quotient of a weight below 2^-100 would overflow)
     const bool fits = m > 0x1p-100f && m < INFINITY;
-    scale[0] = fits ? 32760.0f / m : 1.0f;
-    scale[1] = fits ? m / 32760.0f : 1.0f;
+    rs.scale[0] = fits ? 32760.0f / m : 1.0f;
+    rs.scale[1] = fits ? m / 32760.0f : 1.0f;
 }
 
-// dst[c][r] = src[r][c] for r < R, zero for R <= r < pitch (and for rows whose weight is zero).
-__global__ void __launch_bounds__(256) transpose_kernel(const uint16_t* src, int64_t ld, int R, int C, uint16_t* dst,
-                                                        int pitch, const float* weight) {
+// dst[c][r] = src[r][c] for r < R, zero for R <= r < pitch and for rows that do not count (X of a RowState).
+struct Transpose {
+    const uint16_t* src;
+    uint16_t* dst;
+    int R, C, pitch;       // C the source's pitch, a multiple of 8, as pitch is
+    int tiles_r, tiles;    // 64 x 64 tiles along r, in all (0: nothing to do)
+};
+
+__device__ __forceinline__ void transpose_tile(const Transpose& a, int tile_id, const RowState* rows) {
     __shared__ __attribute__((aligned(16))) uint16_t tile[64][72];
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int r0 = tile_id % a.tiles_r * 64, c0 = tile_id / a.tiles_r * 64;
     const int tid = threadIdx.x;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int r = r0 + (tid >> 3) + 32 * j, c = c0 + 8 * (tid & 7);
         u32x4 v{0, 0, 0, 0};
-        if (r < R && c < C && !(weight && weight[r] == 0.0f))
-            v = *reinterpret_cast<const u32x4*>(src + (int64_t)r * ld + c);
+        if (r < a.R && c < a.C && !(rows && row_weight(*rows, r) == 0.0f))
+            v = *reinterpret_cast<const u32x4*>(a.src + (int64_t)r * a.C + c);
         *reinterpret_cast<u32x4*>(&tile[(tid >> 3) + 32 * j][8 * (tid & 7)]) = v;
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int c = c0 + (tid >> 3) + 32 * j, r = r0 + 8 * (tid & 7);
-        if (c >= C || r >= pitch) continue;
+        if (c >= a.C || r >= a.pitch) continue;
         uint16_t o[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = tile[8 * (tid & 7) + e][(tid >> 3) + 32 * j];
         u32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = o[2 * e] | (uint32_t)o[2 * e + 1] << 16;
-        *reinterpret_cast<u32x4*>(dst + (int64_t)c * pitch + r) = v;
+        *reinterpret_cast<u32x4*>(a.dst + (int64_t)c * a.pitch + r) = v;
     }
 }
 
-hipError_t launch_transpose(const uint16_t* src, int64_t ld, int R, int C, uint16_t* dst, int pitch, const float* weight,
-                            hipStream_t st) {
-    transpose_kernel<<<dim3((unsigned)((pitch + 63) / 64), (unsigned)((C + 63) / 64)), 256, 0, st>>>(src, ld, R, C, dst,
-                                                                                              pitch, weight);
-    return hipGetLastError();
+// What the gradient's products need beside the logits, in one launch: the transposed inputs (rows that do not
+// count left out: zeros times what they hold may not reach dW), a piece's transposed head rows, the scale.
+__global__ void __launch_bounds__(256) prepare_kernel(Transpose x, Transpose w, RowState rs, int n) {
+    const int b = (int)blockIdx.x;
+    if (b < x.tiles) transpose_tile(x, b, &rs);
+    else if (b < x.tiles + w.tiles) transpose_tile(w, b - x.tiles, nullptr);
+    else find_scale(rs, n);
+}
+
+Transpose make_transpose(const uint16_t* src, uint16_t* dst, int R, int C, int pitch) {
+    const int tr = (pitch + 63) / 64;
+    return Transpose{src, dst, R, C, pitch, tr, tr * ((C + 63) / 64)};
 }
 
 int round_up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
@@ -452,7 +476,7 @@ int round_up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
 template <int DT>
 static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W, const RowState& rs, uint16_t* dX,
                                 uint16_t* dW, int n, hipStream_t st) {
-    const int V = L->desc.vocab, F = L->desc.features;
+    const int V = L->desc.vocab, F = L->desc.features, piece = L->piece, np = round_up(n, 8);
     hipError_t e;
     GemmOperands g{};
     g.zero = L->d_zero;
@@ -463,26 +487,35 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     g.ldb = F;
     g.N = n;
     g.K = F;
-    constexpr int WM = 2, WN = 4, AM = 4, AN = 2;
-    if ((e = launch_gemm<DT, WM, WN, AM, AN>(g, StatsEpilogue<WM, WN, AM, AN>{L->d_part, rs}, st)) != hipSuccess) return e;
-    join_kernel<<<(unsigned)((n + 63) / 64), 256, 0, st>>>(rs, L->d_part, (V + 255) / 256, n, V);
+    GemmPlan p = gemm_plan(V, n, F, false);
+    e = p.big ? launch_gemm<DT, 2, 4, 4, 2>(g, p, StatsEpilogue<2, 4, 4, 2>{L->d_part, rs}, st)
+              : launch_gemm<DT, 2, 2, 2, 2>(g, p, StatsEpilogue<2, 2, 2, 2>{L->d_part, rs}, st);
+    if (e != hipSuccess) return e;
+    const int side = p.big ? 256 : 128;
+    join_kernel<<<(unsigned)((n + 15) / 16), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
     if ((e = hipGetLastError()) != hipSuccess || (!dX && !dW)) return e;
-    scale_kernel<<<1, 1024, 0, st>>>(rs.w, n, rs.scale);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int np = round_up(n, 8), piece = L->piece;
-    if (dW && (e = launch_transpose(X, F, n, F, L->d_xt, np, rs.w, st)) != hipSuccess) return e;
+    const GemmPlan px = gemm_plan(n, F, std::min(V, piece), true);
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
         const int rows = (int)std::min<int64_t>(piece, V - v0), rp = round_up(rows, 8);
+        const bool first = v0 == 0, last = v0 + piece >= V;
+        const Transpose tx = first && dW ? make_transpose(X, L->d_xt, n, F, np) : Transpose{};
+        const Transpose tw = dX ? make_transpose(W + v0 * F, L->d_wt, rows, F, piece) : Transpose{};
+        const unsigned blocks = (unsigned)(tx.tiles + tw.tiles + (first ? 1 : 0));
+        if (blocks) prepare_kernel<<<blocks, 256, 0, st>>>(tx, tw, rs, n);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
         g.A = W + v0 * F;
         g.lda = g.ldb = F;
         g.M = rows;
         g.B = X;
         g.N = n;
         g.K = F;
-        GradEpilogue<DT, WM, WN, AM, AN> ge{dX ? L->d_dl : nullptr, dW ? L->d_dlt : nullptr, piece, np, v0, rs};
-        if ((e = launch_gemm<DT, WM, WN, AM, AN>(g, ge, st)) != hipSuccess) return e;
+        p = gemm_plan(rows, n, F, false);
+        uint16_t *dl = dX ? L->d_dl : nullptr, *dlt = dW ? L->d_dlt : nullptr;
+        e = p.big ? launch_gemm<DT, 2, 4, 4, 2>(g, p, GradEpilogue<DT, 2, 4, 4, 2>{dl, dlt, piece, np, v0, rs}, st)
+                  : launch_gemm<DT, 2, 2, 2, 2>(g, p, GradEpilogue<DT, 2, 2, 2, 2>{dl, dlt, piece, np, v0, rs}, st);
+        if (e != hipSuccess) return e;
         if (dX) {
-            if ((e = launch_transpose(W + v0 * F, F, rows, F, L->d_wt, piece, nullptr, st)) != hipSuccess) return e;
+            // dX adds up over the pieces, and over the splits of each
             GemmOperands d = g;
             d.A = L->d_dl;
             d.B = L->d_wt;
@@ -490,9 +523,12 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.M = n;
             d.N = F;
             d.K = rp;
-            const bool last = v0 + piece >= V;
-            StoreEpilogue<DT, WM, WN, AM, AN> se{last ? dX : nullptr, L->d_dx, F, v0 == 0, rs.scale + 1};
-            if ((e = launch_gemm<DT, WM, WN, AM, AN>(d, se, st)) != hipSuccess) return e;
+            const bool whole = px.splits == 1 && last;
+            const int mode = whole ? (first ? STORE_OUT : STORE_LAST) : (first ? STORE_SUM : STORE_ADD);
+            if ((e = launch_store_gemm<DT>(d, px, StoreArgs<DT>{dX, L->d_dx, F, rs.scale + 1}, mode, st)) != hipSuccess)
+                return e;
+            if (last && !whole && (e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.scale + 1, st)) != hipSuccess)
+                return e;
         }
         if (dW) {
             GemmOperands d = g;
@@ -502,8 +538,9 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.M = rows;
             d.N = F;
             d.K = np;
-            StoreEpilogue<DT, WM, WN, AM, AN> se{dW + v0 * F, nullptr, F, 1, rs.scale + 1};
-            if ((e = launch_gemm<DT, WM, WN, AM, AN>(d, se, st)) != hipSuccess) return e;
+            if ((e = launch_store_gemm<DT, STORE_OUT>(d, gemm_plan(rows, F, np, false),
+                                                      StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.scale + 1}, st)) != hipSuccess)
+                return e;
         }
     }
     return hipSuccess;
@@ -535,6 +572,19 @@ aq_status alloc(T** p, size_t bytes, const char* what) {
     return api_hip_fail(e, what);
 }
 
+// Bytes of the input gradient's fp32 sums: the most that a call of any token count takes (its plan has no
+// splits past 512 tiles, and changes at multiples of 128 tokens).
+size_t dx_bytes(const aq_loss* L) {
+    const int64_t mt = L->desc.max_tokens, F = L->desc.features;
+    size_t need = L->piece < L->desc.vocab ? (size_t)mt * F * 4 : 16;
+    for (int64_t n = 128; n < mt + 128 && n <= 128 * 512; n += 128) {
+        const int64_t t = std::min(n, mt);
+        const aq::GemmPlan p = aq::gemm_plan(t, F, std::min<int64_t>(L->desc.vocab, L->piece), true);
+        if (p.splits > 1) need = std::max(need, (size_t)p.splits * t * F * 4);
+    }
+    return need;
+}
+
 // The gradients' workspace (the first call that asks for one allocates it).
 aq_status grad_workspace(aq_loss* L, bool dx, bool dw) {
     const size_t n = (size_t)(L->desc.max_tokens + 7) / 8 * 8, F = (size_t)L->desc.features, P = (size_t)L->piece;
@@ -542,7 +592,7 @@ aq_status grad_workspace(aq_loss* L, bool dx, bool dw) {
     if (dx) {
         s = alloc(&L->d_dl, n * P * 2, "gradient workspace");
         if (s == AQ_OK) s = alloc(&L->d_wt, F * P * 2, "gradient workspace");
-        if (s == AQ_OK && L->piece < L->desc.vocab) s = alloc(&L->d_dx, n * F * 4, "gradient workspace");
+        if (s == AQ_OK) s = alloc(&L->d_dx, dx_bytes(L), "gradient workspace");
     }
     if (s == AQ_OK && dw) s = alloc(&L->d_dlt, n * P * 2, "gradient workspace");
     if (s == AQ_OK && dw) s = alloc(&L->d_xt, n * F * 2, "gradient workspace");
@@ -597,7 +647,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
                                                                               desc->max_tokens, desc->features)));
         const int64_t pieces = (desc->vocab + most - 1) / most;
         L->piece = (int)(((desc->vocab + pieces - 1) / pieces + 255) / 256 * 256);
-        const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 255) / 256;
+        const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 127) / 128;
         aq_status s = alloc(&L->d_zero, 256, "zero block");
         if (s == AQ_OK) s = alloc(&L->d_part, tiles * n * sizeof(float2), "row statistics");
         if (s == AQ_OK) s = alloc(&L->d_row, (4 * n + 2) * sizeof(float), "row state");

@@ -40,6 +40,7 @@ struct aq_usq {
     int sum_groups;
     // input gradient, allocated by its first call
     uint16_t* d_wt;        // [slab][Cp] decoded weights of a slab of inputs, transposed
+    float* d_dsum;         // a K split's partial sums
     uint16_t* d_dy;        // [max_tokens][Cp] output gradient with rows of whole 16-byte groups (C_out % 8 != 0)
     int slab, cp;
 };
@@ -610,7 +611,6 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* src, int 
 
 template <int DT>
 hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uint16_t* dX, int n, hipStream_t st) {
-    constexpr int WM = 2, WN = 4, AM = 4, AN = 2;
     const int K = a.K, C = a.C_out, cp = L->cp;
     hipError_t e;
     GemmOperands g{};
@@ -625,19 +625,21 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
         }
         g.A = L->d_dy;
     }
-    g.lda = C % 8 ? cp : C;
+    g.lda = g.ldb = g.K = cp;
     g.M = n;
     g.B = L->d_wt;
-    g.ldb = cp;
-    g.K = C % 8 ? cp : C;
     for (int k0 = 0; k0 < K; k0 += L->slab) {
         const int cols = std::min(L->slab, K - k0);
         usq_decode_t_kernel<DT><<<dim3((unsigned)((cols + 127) / 128), (unsigned)((cp + 63) / 64)), 256, 0, st>>>(
             a, L->desc.group, k0 / 128, L->d_wt, cp);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         g.N = cols;
-        StoreEpilogue<DT, WM, WN, AM, AN> se{dX + k0, nullptr, K, 1, nullptr};
-        if ((e = launch_gemm<DT, WM, WN, AM, AN>(g, se, st)) != hipSuccess) return e;
+        const GemmPlan p = gemm_plan(n, cols, cp, true);
+        const StoreArgs<DT> s{dX + k0, L->d_dsum, K, nullptr};
+        if ((e = launch_store_gemm<DT>(g, p, s, p.splits > 1 ? STORE_SUM : STORE_OUT, st)) != hipSuccess) return e;
+        if (p.splits > 1 &&
+            (e = launch_split_sum<DT>(L->d_dsum, p.splits, n, cols, dX + k0, K, nullptr, st)) != hipSuccess)
+            return e;
     }
     return hipSuccess;
 }
@@ -649,7 +651,7 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
 namespace {
 
 void free_usq(aq_usq* L) {
-    void* ptrs[] = {L->d_codes, L->d_scales, L->d_zeros, L->d_zero, L->d_sums, L->d_part, L->d_wt, L->d_dy};
+    void* ptrs[] = {L->d_codes, L->d_scales, L->d_zeros, L->d_zero, L->d_sums, L->d_part, L->d_wt, L->d_dsum, L->d_dy};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     delete L;
@@ -734,6 +736,22 @@ aq_status check_call(const aq_usq* L, const void* in, const void* out, int64_t n
     return AQ_OK;
 }
 
+// Bytes of the input gradient's split sums: the most that a call of any token count takes (its plan has no
+// splits past 512 tiles, and changes at multiples of 128 tokens).
+size_t dsum_bytes(const aq_usq* L) {
+    const int64_t mt = L->desc.max_tokens;
+    const int tail = L->desc.in_features % L->slab;
+    size_t need = 16;
+    for (int64_t n = 128; n < mt + 128 && n <= 128 * 512; n += 128)
+        for (const int64_t cols : {std::min(L->slab, L->desc.in_features), tail}) {
+            if (!cols) continue;
+            const int64_t t = std::min(n, mt);
+            const aq::GemmPlan p = aq::gemm_plan(t, cols, L->cp, true);
+            if (p.splits > 1) need = std::max(need, (size_t)p.splits * t * cols * 4);
+        }
+    return need;
+}
+
 aq::UsqArgs make_args(const aq_usq* L, const void* X, void* Y, int64_t n) {
     return aq::UsqArgs{L->d_codes, L->d_scales, L->d_zeros, static_cast<const uint16_t*>(X), Y, L->desc.y_dtype,
                        (int)n, L->desc.in_features, L->desc.out_features, L->nchunk, L->groups,
@@ -809,6 +827,7 @@ aq_status aq_usq_input_grad(aq_usq* L, const void* dY, void* dX, int64_t n, void
         L->slab = (int)std::min<int64_t>(most, (int64_t)L->nchunk * 128);
     }
     s = alloc(&L->d_wt, (size_t)L->slab * L->cp * 2, "gradient workspace");
+    if (s == AQ_OK) s = alloc(&L->d_dsum, dsum_bytes(L), "gradient workspace");
     if (s == AQ_OK && C % 8 != 0) s = alloc(&L->d_dy, (size_t)L->desc.max_tokens * L->cp * 2, "gradient workspace");
     if (s != AQ_OK) return s;
     const aq::UsqArgs a = make_args(L, nullptr, nullptr, n);
