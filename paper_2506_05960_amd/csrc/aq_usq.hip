@@ -143,87 +143,222 @@ __device__ __forceinline__ void store_y3(void* Y, int y_dtype, int64_t i, float 
 
 constexpr int kFewTokens = 64;
 
-// 16 output rows x 16 NT tokens a workgroup; its waves share K chunk by chunk
-// and add their sums in LDS in wave order.  SG: steps of 32 inputs a scale
-// group (group 32, 64, and 128 or more).  S_j comes from a product with ones,
-// which delivers it in the accumulators' own layout.
-template <int DT, int SG, int NT>
-__global__ void __launch_bounds__(512) usq_few_kernel(UsqArgs a) {
-    __shared__ floatx4 red[8][NT][64];
+// 16 RT output rows x 16 NT tokens a workgroup; its waves share K chunk by
+// chunk and add their sums in LDS in wave order.  SG: steps of 32 inputs a
+// scale group (group 32, 64, and 128 or more).  S_j comes from a product with
+// ones, which delivers it in the accumulators' own layout.
+//  * STAGE false (up to four tokens): the tokens are read in the operands' own
+//    layout, and a wave has U chunks' loads on their way at a time.
+//  * STAGE true: that layout puts neighbouring lanes on different tokens, and a
+//    load of sixteen tokens then takes a cycle a lane.  The tokens reach a
+//    buffer of the wave's own in LDS in runs of 64 bytes instead (four lanes a
+//    token, pieces permuted so that sixteen tokens' reads lie in different
+//    banks), a chunk ahead: four times as fast.
+template <int DT, int SG, int NT, int RT, int U, int WAVES, bool STAGE>
+__global__ void __launch_bounds__(WAVES * 64) usq_few_kernel(UsqArgs a) {
+    static_assert(!STAGE || U == 1, "one chunk ahead");
+    constexpr int GPC = 4 / SG;
+    extern __shared__ __attribute__((aligned(16))) uint8_t few_lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
     const int l16 = lane & 15, o = lane >> 4;
-    const int rt = blockIdx.x;
-    const uint16_t* x[NT];
+    const int tiles = (a.C_out + 15) >> 4;
+    const u32x4* codes[RT];
+    int64_t srow[RT];
 #pragma unroll
-    for (int m = 0; m < NT; ++m) x[m] = a.X + (int64_t)min(16 * m + l16, a.n - 1) * a.K + 8 * o;
-    const u32x4* codes = reinterpret_cast<const u32x4*>(a.codes) + (int64_t)rt * a.nchunk * 64 + lane;
-    const int64_t srow = (int64_t)rt * a.groups * 16 + l16;
+    for (int y = 0; y < RT; ++y) {
+        const int64_t rt = min((int)blockIdx.x * RT + y, tiles - 1);      // (a repeated tile's rows are not stored)
+        codes[y] = reinterpret_cast<const u32x4*>(a.codes) + rt * a.nchunk * 64 + lane;
+        srow[y] = rt * a.groups * 16 + l16;
+    }
     const uint32_t one = DT == AQ_BF16 ? 0x3f803f80u : 0x3c003c00u;
     const u32x4 ones{one, one, one, one};
-    floatx4 acc[NT];
+    floatx4 acc[RT][NT];
 #pragma unroll
-    for (int m = 0; m < NT; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int c = wave; c < a.nchunk; c += waves) {
-        const u32x4 w = codes[(int64_t)c * 64];
-        u32x4 xv[4][NT];
+    for (int y = 0; y < RT; ++y)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int k = c * 128 + 32 * s;
+        for (int m = 0; m < NT; ++m) acc[y][m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    u32x4 w[U][RT];
+    uint16_t sc[U][RT][GPC], zp[U][RT][GPC];
+    auto load_weights = [&](int u, int c) {
 #pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                xv[s][m] = u32x4{0, 0, 0, 0};
-                if (k + 8 * o < a.K) xv[s][m] = *reinterpret_cast<const u32x4*>(x[m] + k);
+        for (int y = 0; y < RT; ++y) {
+            w[u][y] = codes[y][(int64_t)c * 64];
+#pragma unroll
+            for (int g = 0; g < GPC; ++g) {
+                const int64_t at = srow[y] + (int64_t)(GPC == 1 ? c / a.per : c * GPC + g) * 16;
+                sc[u][y][g] = a.scales[at];
+                zp[u][y][g] = a.zeros ? a.zeros[at] : 8;
             }
         }
+    };
+    // one chunk's products: its codes, scales and zero points, and its tokens
+    auto chunk = [&](const u32x4 (&cw)[RT], const uint16_t (&cs)[RT][GPC], const uint16_t (&cz)[RT][GPC],
+                     const u32x4 (&xv)[4][NT]) {
 #pragma unroll
-        for (int g = 0; g < 4 / SG; ++g) {
-            const int j = SG == 4 ? c / a.per : c * (4 / SG) + g;
-            const float sc = widen16<DT>(a.scales[srow + (int64_t)j * 16]);
-            const float z = a.zeros ? (float)a.zeros[srow + (int64_t)j * 16] : 8.0f;
-            floatx4 d[NT], xs[NT];
+        for (int g = 0; g < GPC; ++g) {
+            floatx4 xs[NT];
 #pragma unroll
-            for (int m = 0; m < NT; ++m) d[m] = xs[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int m = 0; m < NT; ++m) {
+                xs[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int s = g * SG; s < (g + 1) * SG; ++s) {
-                const u32x4 q = widen_codes<DT>(w[s]);
+                for (int s = g * SG; s < (g + 1) * SG; ++s) xs[m] = mfma16<DT>(xv[s][m], ones, xs[m]);
+            }
+#pragma unroll
+            for (int y = 0; y < RT; ++y) {
+                floatx4 d[NT];
+#pragma unroll
+                for (int m = 0; m < NT; ++m) d[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = g * SG; s < (g + 1) * SG; ++s) {
+                    const u32x4 q = widen_codes<DT>(cw[y][s]);
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) d[m] = mfma16<DT>(xv[s][m], q, d[m]);
+                }
+                const float sf = widen16<DT>(cs[y][g]), z = (float)cz[y][g];
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[y][m][r] = __builtin_fmaf(sf, __builtin_fmaf(-z, xs[m][r], d[m][r]), acc[y][m][r]);
+            }
+        }
+    };
+
+    if constexpr (STAGE) {
+        uint8_t* buf = few_lds + wave * NT * 4096;      // [token block][step][token][four pieces of 16 bytes]
+        const int tok = lane >> 2, piece = (lane & 3) ^ ((tok >> 2) & 3);
+        const __amdgpu_buffer_rsrc_t rx = buffer_rsrc(a.X, 0xFFFFFFFFu);
+        uint32_t ox[NT];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) ox[m] = ((uint32_t)min(16 * m + tok, a.n - 1) * (uint32_t)a.K + 8u * piece) * 2u;
+        auto issue = [&](int c) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
-                    d[m] = mfma16<DT>(xv[s][m], q, d[m]);
-                    xs[m] = mfma16<DT>(xv[s][m], ones, xs[m]);
+                    uint8_t* dst = buf + (m * 4 + s) * 1024;
+                    const int k = c * 128 + 32 * s;
+                    if (c * 128 + 128 <= a.K) {
+                        lds_dma16(rx, ox[m], (uint32_t)k * 2u, dst);
+                    } else {
+                        const uint8_t* p = reinterpret_cast<const uint8_t*>(a.X + k) + ox[m];
+                        lds_dma16(k + 8 * piece < a.K ? p : a.zero, dst);
+                    }
+                }
+        };
+        const uint32_t at = (uint32_t)(l16 * 64 + ((o ^ ((l16 >> 2) & 3)) * 16));
+        if (wave < a.nchunk) {
+            issue(wave);
+            load_weights(0, wave);
+        }
+        for (int c = wave; c < a.nchunk; c += waves) {
+            wait_vmcnt<0>();
+            u32x4 xv[4][NT], cw[RT];
+            uint16_t cs[RT][GPC], cz[RT][GPC];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int m = 0; m < NT; ++m) xv[s][m] = *reinterpret_cast<const u32x4*>(buf + (m * 4 + s) * 1024 + at);
+#pragma unroll
+            for (int y = 0; y < RT; ++y) {
+                cw[y] = w[0][y];
+#pragma unroll
+                for (int g = 0; g < GPC; ++g) {
+                    cs[y][g] = sc[0][y][g];
+                    cz[y][g] = zp[0][y][g];
+                }
+            }
+            if (c + waves < a.nchunk) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the buffer is read: the next chunk may land
+                issue(c + waves);
+                load_weights(0, c + waves);
+            }
+            chunk(cw, cs, cz, xv);
+        }
+        __syncthreads();                                // the buffers become the sums' below
+    } else {
+        const uint16_t* x[NT];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) x[m] = a.X + (int64_t)min(16 * m + l16, a.n - 1) * a.K + 8 * o;
+        for (int c0 = wave; c0 < a.nchunk; c0 += U * waves) {
+            u32x4 xv[U][4][NT];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * waves;
+                load_weights(u, min(c, a.nchunk - 1));
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int k = c * 128 + 32 * s;
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) {
+                        xv[u][s][m] = u32x4{0, 0, 0, 0};                   // past K (and past the last chunk): nothing
+                        if (k + 8 * o < a.K) xv[u][s][m] = *reinterpret_cast<const u32x4*>(x[m] + k);
+                    }
                 }
             }
 #pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    acc[m][r] = __builtin_fmaf(sc, __builtin_fmaf(-z, xs[m][r], d[m][r]), acc[m][r]);
+            for (int u = 0; u < U; ++u) chunk(w[u], sc[u], zp[u], xv[u]);
         }
     }
+    floatx4* red = reinterpret_cast<floatx4*>(few_lds);      // [wave][row tile][token block][lane]
 #pragma unroll
-    for (int m = 0; m < NT; ++m) red[wave][m][lane] = acc[m];
+    for (int y = 0; y < RT; ++y)
+#pragma unroll
+        for (int m = 0; m < NT; ++m) red[((wave * RT + y) * NT + m) * 64 + lane] = acc[y][m];
     __syncthreads();
-    const int i = rt * 16 + l16;
-    for (int m = wave; m < NT; m += waves) {
-        floatx4 v = red[0][m][lane];
-        for (int w = 1; w < waves; ++w) v += red[w][m][lane];
+    for (int ym = wave; ym < RT * NT; ym += waves) {
+        floatx4 v = red[ym * 64 + lane];
+        for (int w = 1; w < waves; ++w) v += red[(w * RT * NT + ym) * 64 + lane];
+        const int rt = blockIdx.x * RT + ym / NT, i = rt * 16 + l16;
         if (i >= a.C_out) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int tok = 16 * m + 4 * o + r;
+            const int tok = 16 * (ym % NT) + 4 * o + r;
             if (tok < a.n) store_y3(a.Y, a.y_dtype, (int64_t)tok * a.C_out + i, v[r]);
         }
     }
 }
 
+template <int DT, int SG, int NT, int RT, int U, int WAVES, bool STAGE>
+hipError_t launch_few(const UsqArgs& a, hipStream_t st) {
+    const unsigned grid = (unsigned)((a.C_out + 16 * RT - 1) / (16 * RT));
+    const int waves = std::min(WAVES, a.nchunk);
+    const size_t lds = (size_t)waves * NT * std::max(STAGE ? 4096 : 0, RT * 1024);
+    auto kern = usq_few_kernel<DT, SG, NT, RT, U, WAVES, STAGE>;
+    const hipError_t e = ensure_dynamic_lds((const void*)kern, lds);
+    if (e != hipSuccess) return e;
+    kern<<<grid, waves * 64, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+// Output rows a workgroup (16 RT): more of them share the tokens' reads, fewer fill the chip.  us, RT = 1 / 2 / 4:
+//   4096 -> 16384:   1 token  9.2 / 7.3 / 7.7    16 tokens 11.9 / 9.5 / 9.8    32: 21.6 / 15.8 / 13.0
+//                   64 tokens 43.4 / 28.1 / 20.7
+//   4096 -> 4096:    1 token  5.9 / 5.7 / 6.8    32 tokens 7.3 / 7.6 / 9.4     64: 12.2 / 11.2 / 14.7
+//   16384 -> 4096:   1 token 10.5 / 13.3 / 20.8  16 tokens 13.1 / 16.8 / 25.3  64: 38.4 / 36.2 / 49.6
+// Long reductions in few row tiles take sixteen waves: 16384 -> 4096, 1 token 10.5 -> 9.1, 16 tokens 13.1 -> 12.4.
 template <int DT, int SG>
 hipError_t launch_few(const UsqArgs& a, hipStream_t st) {
-    const int waves = std::min(8, a.nchunk);
-    const dim3 grid((unsigned)((a.C_out + 15) / 16));
-    if (a.n <= 16) usq_few_kernel<DT, SG, 1><<<grid, waves * 64, 0, st>>>(a);
-    else if (a.n <= 32) usq_few_kernel<DT, SG, 2><<<grid, waves * 64, 0, st>>>(a);
-    else usq_few_kernel<DT, SG, 4><<<grid, waves * 64, 0, st>>>(a);
-    return hipGetLastError();
+    const int tiles = (a.C_out + 15) / 16;
+    if (a.n <= 16) {
+        const bool long_few = tiles < 512 && a.nchunk >= 64;
+        if (a.n <= 4)
+            return tiles >= 512 ? launch_few<DT, SG, 1, 2, 2, 8, false>(a, st)
+                   : long_few   ? launch_few<DT, SG, 1, 1, 2, 16, false>(a, st)
+                                : launch_few<DT, SG, 1, 1, 2, 8, false>(a, st);
+        return tiles >= 512 ? launch_few<DT, SG, 1, 2, 1, 8, true>(a, st)
+               : long_few   ? launch_few<DT, SG, 1, 1, 1, 16, true>(a, st)
+                            : launch_few<DT, SG, 1, 1, 1, 8, true>(a, st);
+    }
+    if (a.n <= 32)
+        return tiles >= 1024  ? launch_few<DT, SG, 2, 4, 1, 8, true>(a, st)
+               : tiles >= 300 ? launch_few<DT, SG, 2, 2, 1, 8, true>(a, st)
+                              : launch_few<DT, SG, 2, 1, 1, 8, true>(a, st);
+    if constexpr (SG == 4)      // (groups below 128 have too many values to hold)
+        if (tiles >= 768) return launch_few<DT, SG, 4, 4, 1, 8, true>(a, st);
+    return tiles >= 256 ? launch_few<DT, SG, 4, 2, 1, 8, true>(a, st) : launch_few<DT, SG, 4, 1, 1, 8, true>(a, st);
 }
 
 // ---- many tokens ----
