@@ -19,9 +19,7 @@ struct aq_loss {
     float2* d_part;        // [vocabulary tile of 128][max_tokens] maximum and sum of exponentials
     float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then {scale, 1 / scale}
     // gradient workspace, allocated by the first call that needs it
-    uint16_t* d_dl;        // [max_tokens][piece] logits' gradient of a piece
-    uint16_t* d_dlt;       // [piece][tokens] the same, transposed
-    uint16_t* d_wt;        // [features][piece] the piece's head rows, transposed
+    uint16_t* d_dlt;       // [piece][tokens] logits' gradient of a piece
     uint16_t* d_xt;        // [features][tokens] inputs, transposed
     float* d_dx;           // [max_tokens][features] input gradient of the pieces so far
 };
@@ -360,46 +358,49 @@ struct StatsEpilogue {
 };
 
 // dloss (P - 1 at the target) of a piece of the vocabulary, in 16 bits, as
-// [token][row] and as [row][token].  Tokens up to a multiple of 8 and rows up
-// to the tile's end are written (zeros past the ends): the products that read
-// them walk whole 16-byte groups.
+// [row][token].  Tokens up to a multiple of 8 and rows up to the tile's end are
+// written (zeros past the ends): the products that read them walk whole 16-byte
+// groups.  Neighbouring lanes hold neighbouring tokens: each pair of lanes swaps
+// half of its values, so that every store carries two tokens of a row.
 template <int DT, int WM, int WN, int AM, int AN>
 struct GradEpilogue {
-    uint16_t* dl;          // [n][piece], or null
-    uint16_t* dlt;         // [piece][np], or null
-    int piece, np;         // pitches
+    uint16_t* dlt;         // [piece][np]
+    int piece, np;
     int64_t v0;            // first vocabulary row of the piece
     RowState rs;
     __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int, int m0, int n0, int M, int N, uint8_t*) const {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
         const float scale = rs.scale[0];
+        const bool odd = lane & 1;
+        // the tile's rows from its corner: at most 255 pitches of kMaxPitch
+        const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(dlt + (int64_t)m0 * np + n0, kOutOfRange);
 #pragma unroll
         for (int b = 0; b < AN; ++b) {
-            const int t = n0 + wn * AN * 32 + b * 32 + l32;
+            const int col = wn * AN * 32 + b * 32 + l32, t = n0 + col;
             const int64_t tv = t < N ? rs.targets[t] - v0 : -1;
-            const int target = tv >= 0 && tv < M ? (int)tv : -1;
+            const int target = tv >= 0 && tv < M ? (int)tv - m0 : -1;
             const float top = t < N ? rs.top[t] : 0.0f, ls = t < N ? rs.ls[t] : 0.0f;
             const float w = t < N ? rs.w[t] * scale : 0.0f;
 #pragma unroll
             for (int a = 0; a < AM; ++a)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int v = m0 + (wm * AM + a) * 32 + 8 * q + 4 * hi;
-                    uint16_t o[4];
+                for (int r = 0; r < 16; r += 2) {
+                    const int v = (wm * AM + a) * 32 + gemm_row(r, hi);        // rows v and v + 1
+                    uint32_t o[2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float p = exp2_fast(__builtin_fmaf(acc[a][b][4 * q + e] - top, kLog2e, -ls));
+                    for (int e = 0; e < 2; ++e) {
+                        float p = exp2_fast(__builtin_fmaf(acc[a][b][r + e] - top, kLog2e, -ls));
                         if (v + e == target) p -= 1.0f;
-                        o[e] = f32_to_tile<DT>(v + e < M && w != 0.0f ? p * w : 0.0f);
+                        o[e] = f32_to_tile<DT>(m0 + v + e < M && w != 0.0f ? p * w : 0.0f);
                     }
-                    if (dl && t < N && v < piece)
-                        *reinterpret_cast<uint2*>(dl + (int64_t)t * piece + v) =
-                            make_uint2(o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16);
-                    if (dlt && t < np && v < piece) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) dlt[(int64_t)(v + e) * np + t] = o[e];
-                    }
+                    // even lanes keep row v of both tokens, odd lanes row v + 1
+                    const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? o[0] : o[1]), 0xB1, 0xF, 0xF, true);
+                    const uint32_t two = odd ? got | o[1] << 16 : o[0] | got << 16;
+                    const int row = v + (odd ? 1 : 0);
+                    const bool in = (t & ~1) < np && m0 + row < piece;
+                    __builtin_amdgcn_raw_buffer_store_b32(
+                        two, ro, in ? (uint32_t)(row * np + (col & ~1)) * 2u : kOutOfRange, 0, 0);
                 }
         }
     }
@@ -463,7 +464,7 @@ __device__ __forceinline__ void find_scale(const RowState& rs, int n) {
     rs.scale[1] = fits ? m / 32760.0f : 1.0f;
 }
 
-// dst[c][r] = src[r][c] for r < R, zero for R <= r < pitch and for rows that do not count (X of a RowState).
+// dst[c][r] = src[r][c] for r < R, zero for R <= r < pitch and for rows that do not count.
 struct Transpose {
     const uint16_t* src;
     uint16_t* dst;
@@ -471,7 +472,7 @@ struct Transpose {
     int tiles_r, tiles;    // 64 x 64 tiles along r, in all (0: nothing to do)
 };
 
-__device__ __forceinline__ void transpose_tile(const Transpose& a, int tile_id, const RowState* rows) {
+__device__ __forceinline__ void transpose_tile(const Transpose& a, int tile_id, const RowState& rows) {
     __shared__ __attribute__((aligned(16))) uint16_t tile[64][72];
     const int r0 = tile_id % a.tiles_r * 64, c0 = tile_id / a.tiles_r * 64;
     const int tid = threadIdx.x;
@@ -479,7 +480,7 @@ __device__ __forceinline__ void transpose_tile(const Transpose& a, int tile_id, 
     for (int j = 0; j < 2; ++j) {
         const int r = r0 + (tid >> 3) + 32 * j, c = c0 + 8 * (tid & 7);
         u32x4 v{0, 0, 0, 0};
-        if (r < a.R && c < a.C && !(rows && row_weight(*rows, r) == 0.0f))
+        if (r < a.R && c < a.C && row_weight(rows, r) != 0.0f)
             v = *reinterpret_cast<const u32x4*>(a.src + (int64_t)r * a.C + c);
         *reinterpret_cast<u32x4*>(&tile[(tid >> 3) + 32 * j][8 * (tid & 7)]) = v;
     }
@@ -498,18 +499,11 @@ __device__ __forceinline__ void transpose_tile(const Transpose& a, int tile_id, 
     }
 }
 
-// What the gradient's products need beside the logits, in one launch: the transposed inputs (rows that do not
-// count left out: zeros times what they hold may not reach dW), a piece's transposed head rows, the scale.
-__global__ void __launch_bounds__(256) prepare_kernel(Transpose x, Transpose w, RowState rs, int n) {
-    const int b = (int)blockIdx.x;
-    if (b < x.tiles) transpose_tile(x, b, &rs);
-    else if (b < x.tiles + w.tiles) transpose_tile(w, b - x.tiles, nullptr);
+// What the gradient's products need beside the logits, in one launch: the scale, and for dW the transposed inputs
+// (rows that do not count left out: zeros times what they hold may not reach dW).
+__global__ void __launch_bounds__(256) prepare_kernel(Transpose x, RowState rs, int n) {
+    if ((int)blockIdx.x < x.tiles) transpose_tile(x, (int)blockIdx.x, rs);
     else find_scale(rs, n);
-}
-
-Transpose make_transpose(const uint16_t* src, uint16_t* dst, int R, int C, int pitch) {
-    const int tr = (pitch + 63) / 64;
-    return Transpose{src, dst, R, C, pitch, tr, tr * ((C + 63) / 64)};
 }
 
 int round_up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
@@ -531,47 +525,44 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     g.N = n;
     g.K = F;
     GemmPlan p = gemm_plan(V, n, F, false);
-    e = p.big ? launch_gemm<DT, 2, 4, 4, 2>(g, p, StatsEpilogue<2, 4, 4, 2>{L->d_part, rs}, st)
-              : launch_gemm<DT, 2, 2, 2, 2>(g, p, StatsEpilogue<2, 2, 2, 2>{L->d_part, rs}, st);
+    e = p.big ? launch_gemm<DT, 2, 4, 4, 2, false>(g, p, StatsEpilogue<2, 4, 4, 2>{L->d_part, rs}, st)
+              : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, StatsEpilogue<2, 2, 2, 2>{L->d_part, rs}, st);
     if (e != hipSuccess) return e;
     const int side = p.big ? 256 : 128;
     join_kernel<<<(unsigned)((n + 15) / 16), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
     if ((e = hipGetLastError()) != hipSuccess || (!dX && !dW)) return e;
+    const int tiles_r = (np + 63) / 64;
+    const Transpose tx = dW ? Transpose{X, L->d_xt, n, F, np, tiles_r, tiles_r * ((F + 63) / 64)} : Transpose{};
+    prepare_kernel<<<(unsigned)tx.tiles + 1, 256, 0, st>>>(tx, rs, n);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     const GemmPlan px = gemm_plan(n, F, std::min(V, piece), true);
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
-        const int rows = (int)std::min<int64_t>(piece, V - v0), rp = round_up(rows, 8);
+        const int rows = (int)std::min<int64_t>(piece, V - v0);
         const bool first = v0 == 0, last = v0 + piece >= V;
-        const Transpose tx = first && dW ? make_transpose(X, L->d_xt, n, F, np) : Transpose{};
-        const Transpose tw = dX ? make_transpose(W + v0 * F, L->d_wt, rows, F, piece) : Transpose{};
-        const unsigned blocks = (unsigned)(tx.tiles + tw.tiles + (first ? 1 : 0));
-        if (blocks) prepare_kernel<<<blocks, 256, 0, st>>>(tx, tw, rs, n);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
         g.A = W + v0 * F;
-        g.lda = g.ldb = F;
         g.M = rows;
-        g.B = X;
-        g.N = n;
-        g.K = F;
         p = gemm_plan(rows, n, F, false);
-        uint16_t *dl = dX ? L->d_dl : nullptr, *dlt = dW ? L->d_dlt : nullptr;
-        e = p.big ? launch_gemm<DT, 2, 4, 4, 2>(g, p, GradEpilogue<DT, 2, 4, 4, 2>{dl, dlt, piece, np, v0, rs}, st)
-                  : launch_gemm<DT, 2, 2, 2, 2>(g, p, GradEpilogue<DT, 2, 2, 2, 2>{dl, dlt, piece, np, v0, rs}, st);
+        e = p.big ? launch_gemm<DT, 2, 4, 4, 2, false>(g, p, GradEpilogue<DT, 2, 4, 4, 2>{L->d_dlt, piece, np, v0, rs}, st)
+                  : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, GradEpilogue<DT, 2, 2, 2, 2>{L->d_dlt, piece, np, v0, rs}, st);
         if (e != hipSuccess) return e;
         if (dX) {
-            // dX adds up over the pieces, and over the splits of each
+            // the sum runs over rows of both operands; dX adds up over the pieces, and over the splits of each
             GemmOperands d = g;
-            d.A = L->d_dl;
-            d.B = L->d_wt;
-            d.lda = d.ldb = piece;
+            d.A = L->d_dlt;
+            d.lda = np;
             d.M = n;
+            d.B = W + v0 * F;
             d.N = F;
-            d.K = rp;
+            d.K = rows;
             const bool whole = px.splits == 1 && last;
-            const int mode = whole ? (first ? STORE_OUT : STORE_LAST) : (first ? STORE_SUM : STORE_ADD);
-            if ((e = launch_store_gemm<DT>(d, px, StoreArgs<DT>{dX, L->d_dx, F, rs.scale + 1}, mode, st)) != hipSuccess)
-                return e;
-            if (last && !whole && (e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.scale + 1, st)) != hipSuccess)
-                return e;
+            const StoreArgs<DT> s{dX, L->d_dx, F, rs.scale + 1};
+            e = whole ? (first ? launch_store_gemm<DT, true, STORE_OUT>(d, px, s, st)
+                               : launch_store_gemm<DT, true, STORE_LAST>(d, px, s, st))
+                      : (first ? launch_store_gemm<DT, true, STORE_SUM>(d, px, s, st)
+                               : launch_store_gemm<DT, true, STORE_ADD>(d, px, s, st));
+            if (e == hipSuccess && last && !whole)
+                e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.scale + 1, st);
+            if (e != hipSuccess) return e;
         }
         if (dW) {
             GemmOperands d = g;
@@ -581,9 +572,9 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.M = rows;
             d.N = F;
             d.K = np;
-            if ((e = launch_store_gemm<DT, STORE_OUT>(d, gemm_plan(rows, F, np, false),
-                                                      StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.scale + 1}, st)) != hipSuccess)
-                return e;
+            e = launch_store_gemm<DT, false, STORE_OUT>(d, gemm_plan(rows, F, np, false),
+                                                        StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.scale + 1}, st);
+            if (e != hipSuccess) return e;
         }
     }
     return hipSuccess;
@@ -603,7 +594,7 @@ static hipError_t distill(const DistillArgs& a, hipStream_t st) {
 namespace {
 
 void free_loss(aq_loss* L) {
-    void* ptrs[] = {L->d_zero, L->d_part, L->d_row, L->d_dl, L->d_dlt, L->d_wt, L->d_xt, L->d_dx};
+    void* ptrs[] = {L->d_zero, L->d_part, L->d_row, L->d_dlt, L->d_xt, L->d_dx};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     delete L;
@@ -635,12 +626,8 @@ size_t dx_bytes(const aq_loss* L) {
 aq_status grad_workspace(aq_loss* L, bool dx, bool dw) {
     const size_t n = (size_t)(L->desc.max_tokens + 7) / 8 * 8, F = (size_t)L->desc.features, P = (size_t)L->piece;
     aq_status s = AQ_OK;
-    if (dx) {
-        s = alloc(&L->d_dl, n * P * 2, "gradient workspace");
-        if (s == AQ_OK) s = alloc(&L->d_wt, F * P * 2, "gradient workspace");
-        if (s == AQ_OK) s = alloc(&L->d_dx, dx_bytes(L), "gradient workspace");
-    }
-    if (s == AQ_OK && dw) s = alloc(&L->d_dlt, n * P * 2, "gradient workspace");
+    s = alloc(&L->d_dlt, n * P * 2, "gradient workspace");
+    if (s == AQ_OK && dx) s = alloc(&L->d_dx, dx_bytes(L), "gradient workspace");
     if (s == AQ_OK && dw) s = alloc(&L->d_xt, n * F * 2, "gradient workspace");
     return s;
 }
@@ -688,7 +675,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
         return api_hip_fail(e, "hipGetDevice");
     }
     if (desc->features) {
-        // a piece's gradient and its transposed head rows take at most 128 MiB each
+        // a piece's gradient takes at most 128 MiB, its head rows too
         const int64_t most = std::min(aq::kMaxPitch / 2, std::max<int64_t>(256, (int64_t(64) << 20) / std::max<int64_t>(
                                                                               desc->max_tokens, desc->features)));
         const int64_t pieces = (desc->vocab + most - 1) / most;

@@ -19,6 +19,7 @@
 // so each group's fp32 sum is scaled once and no weight is ever rounded.
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "aq_gemm.h"
 
@@ -508,7 +509,7 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
 #pragma unroll
         for (int x = 0; x < AM; ++x)
             ps[x] = reinterpret_cast<const u32x4*>(a.sums) + min(m0 + (wm * AM + x) * 32 + l32, a.n - 1);
-#pragma unroll 2
+#pragma unroll 4
         for (int j0 = j_beg; j0 < j_end; j0 += 2) {
             const int j = min(j0 + hi, j_end - 1);
             const bool live = j0 + hi < j_end;
@@ -614,21 +615,37 @@ __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
 #pragma unroll
         for (int b = 0; b < AN; ++b) scale(x, b);
 
-    float* part = a.part ? a.part + (int64_t)z * a.n * a.C_out : nullptr;
+    // branch-free buffer stores at offsets from the tile's corner (past the edge: past the buffer)
+    auto store = [&](void* base, auto bytes, auto&& put) {
+        constexpr int kBytes = decltype(bytes)::value;
+        const __amdgpu_buffer_rsrc_t ry =
+            buffer_rsrc(static_cast<uint8_t*>(base) + ((int64_t)m0 * a.C_out + n0) * kBytes, kOutOfRange);
 #pragma unroll
-    for (int x = 0; x < AM; ++x)
+        for (int x = 0; x < AM; ++x)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int t = m0 + (wm * AM + x) * 32 + gemm_row(r, hi);
-            if (t >= a.n) continue;
+            for (int r = 0; r < 16; ++r) {
+                const int t = (wm * AM + x) * 32 + gemm_row(r, hi);
 #pragma unroll
-            for (int b = 0; b < AN; ++b) {
-                const int i = n0 + (wn * AN + b) * 32 + l32;
-                if (i >= a.C_out) continue;
-                if (part) part[(int64_t)t * a.C_out + i] = acc[x][b][r];
-                else store_y3(a.Y, a.y_dtype, (int64_t)t * a.C_out + i, acc[x][b][r]);
+                for (int b = 0; b < AN; ++b) {
+                    const int i = (wn * AN + b) * 32 + l32;
+                    const bool in = m0 + t < a.n && n0 + i < a.C_out;
+                    put(ry, in ? (uint32_t)(t * a.C_out + i) * (uint32_t)kBytes : kOutOfRange, acc[x][b][r]);
+                }
             }
-        }
+    };
+    auto put32 = [](__amdgpu_buffer_rsrc_t ry, uint32_t off, float v) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), ry, off, 0, 0);
+    };
+    using four = std::integral_constant<int, 4>;
+    using two = std::integral_constant<int, 2>;
+    if (a.part) store(a.part + (int64_t)z * a.n * a.C_out, four{}, put32);
+    else if (a.y_dtype == AQ_F32) store(a.Y, four{}, put32);
+    else if (a.y_dtype == AQ_F16) store(a.Y, two{}, [](__amdgpu_buffer_rsrc_t ry, uint32_t off, float v) {
+        __builtin_amdgcn_raw_buffer_store_b16(f32_to_f16(v), ry, off, 0, 0);
+    });
+    else store(a.Y, two{}, [](__amdgpu_buffer_rsrc_t ry, uint32_t off, float v) {
+        __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(v), ry, off, 0, 0);
+    });
 }
 
 // Y = sum over the K splits, in split order.
@@ -641,23 +658,30 @@ __global__ void __launch_bounds__(256) usq_join_kernel(const float* part, int sp
 }
 
 struct UsqPlan {
-    int am;                // token blocks of 64 a tile
-    int tiles, cps, splits;
+    int tiles, splits, cps;
 };
 
-// Tiles of 256 tokens once they fill the chip, else of 128; K split over
-// workgroups until they do.
+// K splits of a call, shortest by a model fitted to it: a workgroup's fixed
+// time, 1.3 us a chunk alone on its compute unit and 2.3 with a second one,
+// and the partial sums written and read back (256 tokens, 4096 -> 4096: four
+// splits 30 us, eight 36).
 UsqPlan usq_plan(int64_t n, int C_out, int nchunk) {
-    UsqPlan p;
-    const int64_t tn = (C_out + 127) / 128;
-    p.am = 2;
-    const int64_t tiles = (n + 64 * p.am - 1) / (64 * p.am) * tn;
-    p.tiles = (int)tiles;
-    const int most = std::max(1, nchunk / 4);
-    int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / tiles));
-    p.cps = (nchunk + splits - 1) / splits;
-    p.splits = (nchunk + p.cps - 1) / p.cps;
-    return p;
+    const int64_t tiles = (n + 127) / 128 * ((C_out + 127) / 128);
+    UsqPlan best{(int)tiles, 1, nchunk};
+    double best_us = 1e30;
+    for (int s = 1; s <= std::max(1, nchunk / 2) && tiles * s <= std::max<int64_t>(tiles, 512); ++s) {
+        const int cps = (nchunk + s - 1) / s;
+        if ((nchunk + cps - 1) / cps != s) continue;
+        const int64_t wgs = tiles * s;
+        const double work = wgs <= 256 ? 7.0 + 1.3 * cps : (double)((wgs + 511) / 512) * (7.0 + 2.3 * cps);
+        const double us = work + (s > 1 ? 4.5 + 2e-6 * s * n * C_out : 0.0);
+        if (us < best_us) {
+            best_us = us;
+            best.splits = s;
+            best.cps = cps;
+        }
+    }
+    return best;
 }
 
 template <int DT, int SG, int WM, int WN, int AM, int AN>
@@ -771,7 +795,9 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
         g.N = cols;
         const GemmPlan p = gemm_plan(n, cols, cp, true);
         const StoreArgs<DT> s{dX + k0, L->d_dsum, K, nullptr};
-        if ((e = launch_store_gemm<DT>(g, p, s, p.splits > 1 ? STORE_SUM : STORE_OUT, st)) != hipSuccess) return e;
+        e = p.splits > 1 ? launch_store_gemm<DT, false, STORE_SUM>(g, p, s, st)
+                         : launch_store_gemm<DT, false, STORE_OUT>(g, p, s, st);
+        if (e != hipSuccess) return e;
         if (p.splits > 1 &&
             (e = launch_split_sum<DT>(L->d_dsum, p.splits, n, cols, dX + k0, K, nullptr, st)) != hipSuccess)
             return e;
