@@ -325,24 +325,39 @@ struct StatsEpilogue {
             // the target as a row of this lane's first register
             const int64_t tv = t < N ? rs.targets[t] : -1;
             const int target = tv >= 0 && tv < M ? (int)tv - v0 : -1;
-            float m = -INFINITY;
+            // (rarely does a wave's part of the vocabulary hold any of its tokens' targets)
+            if (__any(target >= 0 && target < AM * 32)) {
+                float z = 0.0f;
+                bool mine = false;
 #pragma unroll
-            for (int a = 0; a < AM; ++a)
+                for (int a = 0; a < AM; ++a)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int v = a * 32 + gemm_row(r, 0);
-                    if (!edge || v0 + v < M) m = fmaxf(m, acc[a][b][r]);
-                    if (v == target) rs.zt[t] = acc[a][b][r];
-                }
-            const float bm = m == -INFINITY ? 0.0f : m;
-            float s = 0.0f;
+                    for (int r = 0; r < 16; ++r)
+                        if (a * 32 + gemm_row(r, 0) == target) {
+                            z = acc[a][b][r];
+                            mine = true;
+                        }
+                if (mine) rs.zt[t] = z;
+            }
+            float m = -INFINITY, s = 0.0f;
+            auto reduce = [&](auto last_tile) {
+                constexpr bool kEdge = decltype(last_tile)::value;
 #pragma unroll
-            for (int a = 0; a < AM; ++a)
+                for (int a = 0; a < AM; ++a)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float e = exp2_fast((acc[a][b][r] - bm) * kLog2e);
-                    if (!edge || v0 + a * 32 + gemm_row(r, 0) < M) s += e;
-                }
+                    for (int r = 0; r < 16; ++r)
+                        if (!kEdge || v0 + a * 32 + gemm_row(r, 0) < M) m = fmaxf(m, acc[a][b][r]);
+                const float bm = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int a = 0; a < AM; ++a)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float e = exp2_fast((acc[a][b][r] - bm) * kLog2e);
+                        if (!kEdge || v0 + a * 32 + gemm_row(r, 0) < M) s += e;
+                    }
+            };
+            if (edge) reduce(std::true_type{});
+            else reduce(std::false_type{});
             merge(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32), kLog2e);
             if (hi == 0) red[wm * BN + col] = make_float2(m, s);
         }
@@ -382,6 +397,7 @@ struct GradEpilogue {
             const int target = tv >= 0 && tv < M ? (int)tv - m0 : -1;
             const float top = t < N ? rs.top[t] : 0.0f, ls = t < N ? rs.ls[t] : 0.0f;
             const float w = t < N ? rs.w[t] * scale : 0.0f;
+            const uint32_t live = w != 0.0f ? 0xffffu : 0u;            // (zeros whatever the logits are)
 #pragma unroll
             for (int a = 0; a < AM; ++a)
 #pragma unroll
@@ -392,7 +408,7 @@ struct GradEpilogue {
                     for (int e = 0; e < 2; ++e) {
                         float p = exp2_fast(__builtin_fmaf(acc[a][b][r + e] - top, kLog2e, -ls));
                         if (v + e == target) p -= 1.0f;
-                        o[e] = f32_to_tile<DT>(m0 + v + e < M && w != 0.0f ? p * w : 0.0f);
+                        o[e] = f32_to_tile<DT>(m0 + v + e < M ? p * w : 0.0f) & live;
                     }
                     // even lanes keep row v of both tokens, odd lanes row v + 1
                     const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? o[0] : o[1]), 0xB1, 0xF, 0xF, true);
