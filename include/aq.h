@@ -380,7 +380,8 @@ typedef struct {
  *           AQ_ERR_INVALID_ARGUMENT); NULL: every zero point is 8
  *   out     receives the handle (set to NULL on failure)
  * Formats outside the descriptor's comments that are valid otherwise return
- * AQ_ERR_UNSUPPORTED.  Without a GPU: AQ_ERR_DEVICE.
+ * AQ_ERR_UNSUPPORTED, and so do more than 2^21 features or 2^24 tokens.
+ * Without a GPU: AQ_ERR_DEVICE.
  */
 aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* scales, const uint8_t* zeros,
                         aq_usq** out);
@@ -398,7 +399,8 @@ aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* 
  * Above 64 tokens a call uses the layer's workspace (the inputs' group sums,
  * 16 bytes per token and group, and at most 32 MiB of partial sums, allocated
  * with the layer): serialise such calls on one stream.
- * The layer's device has to be the current one (AQ_ERR_INVALID_ARGUMENT).
+ * X and Y must not overlap.  The layer's device has to be the current one
+ * (AQ_ERR_INVALID_ARGUMENT).
  */
 aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void* stream);
 
@@ -407,10 +409,11 @@ aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void*
  * frozen 4-bit layer.  W is rounded once to desc->dtype, sums are fp32.
  *   dY  device [n][out_features] in desc->dtype; 16-byte aligned
  *   dX  device [n][in_features] in desc->dtype, overwritten; 16-byte aligned
- * The first call on a layer allocates its workspace (synchronous, not under
- * graph capture): the decoded weights of a slab of inputs, at most 32 MiB (or
- * of 128 inputs), and, unless out_features is a multiple of 8, a copy of dY
- * for max_tokens tokens.  Later calls are asynchronous and allocate nothing.
+ * The first call on a layer allocates its workspace (synchronous; refused with
+ * AQ_ERR_UNSUPPORTED on a stream under graph capture): the decoded weights of a
+ * slab of inputs, at most 32 MiB (or of 128 inputs), at most 64 MiB of partial
+ * sums, and, unless out_features is a multiple of 8, a copy of dY for
+ * max_tokens tokens.  Later calls are asynchronous and allocate nothing.
  * Gradients of one layer share that workspace: serialise them on one stream.
  * Errors and determinism as for aq_usq_forward.
  */
@@ -434,7 +437,10 @@ typedef struct {
 } aq_loss_desc;
 
 /* Create the losses of one vocabulary on the current HIP device, with the row
- * statistics of the cross entropy: 8 bytes per token and 256 vocabulary rows. */
+ * statistics of the cross entropy: 8 bytes per token and 128 vocabulary rows.
+ * AQ_ERR_UNSUPPORTED: a vocabulary above 2^30, more than 2^24 tokens, or, for
+ * the cross entropy, more than 2^21 features or tokens.  Every call needs the
+ * handle's device to be the current one (AQ_ERR_INVALID_ARGUMENT). */
 aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
 
 /*
@@ -460,12 +466,15 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
  *   n        1 <= n <= max_tokens
  * Sums are fp32; dz is rounded once to desc->dtype before the products (scaled
  * so that the largest |dloss| lies just below 2^15).
- * The first call with dX or dW allocates their workspace (synchronous, not
- * under graph capture): per token and per feature 2 bytes for each vocabulary
- * row of a piece (at most 128 MiB each, or 256 rows), and copies of X.  Later
- * calls are asynchronous and allocate nothing.  Calls on one handle share its
- * workspace: serialise them on one stream.  Summation orders are fixed:
- * repeated calls give identical bits.
+ * dX and dW must overlap nothing else.
+ * The first call with dX or with dW allocates its workspace (synchronous;
+ * refused with AQ_ERR_UNSUPPORTED on a stream under graph capture): 2 bytes
+ * per token and vocabulary row of a piece (at most 128 MiB, or 256 rows), for
+ * dX fp32 sums (4 bytes per token and feature unless one piece holds the
+ * vocabulary, or up to 64 MiB), for dW a copy of X.  Later calls are
+ * asynchronous and allocate nothing.  Calls on one handle share its workspace:
+ * serialise them on one stream.  Summation orders are fixed: repeated calls
+ * give identical bits.
  */
 aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void* W, const int64_t* targets,
                                 const float* dloss, float* loss, void* dX, void* dW, int64_t n, void* stream);

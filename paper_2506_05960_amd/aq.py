@@ -292,7 +292,8 @@ def _torch_dtypes(name: str):
     if not _TORCH_DTYPES:
         import torch
         _TORCH_DTYPES.update({"f32": (torch.float32,), "f16": (torch.float16,),
-                              "bf16": (torch.bfloat16, torch.int16), "i8": (torch.int8,)})
+                              "bf16": (torch.bfloat16, torch.int16), "i8": (torch.int8,), "i32": (torch.int32,),
+                              "i64": (torch.int64,)})
     return _TORCH_DTYPES[name]
 
 
@@ -514,12 +515,22 @@ class AQLayer:
 
 # ---- 4-bit layers and losses ----
 
+def _need(what: str, t, dtype, shape, device) -> None:
+    """``_check_tensor`` for one dtype, at a fraction of its time where ``t`` fits (a small call's host time counts)."""
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous():
+            return
+    except AttributeError:
+        pass
+    _check_tensor(what, t, (dtype,), shape, device)
+
+
 def _rows(what: str, t) -> int:
-    """Rows of the matrix ``t`` (its other checks come from ``_check_tensor``)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[0] < 1:
+    """Rows of the matrix ``t`` (its other checks come from ``_need``)."""
+    shape = getattr(t, "shape", ())
+    if len(shape) != 2 or shape[0] < 1 or not hasattr(t, "data_ptr"):
         raise ValueError(f"{what} must be a torch matrix with at least one row")
-    return t.shape[0]
+    return shape[0]
 
 
 def _host_array(what: str, a, dtype, shape):
@@ -542,12 +553,21 @@ def _host_array(what: str, a, dtype, shape):
 
 def _output(what: str, out, dtype, shape, device, like):
     """The tensor ``out``, checked, or a new one where it is True; None where it is None or False."""
-    import torch
     if out is None or out is False:
         return None
     if out is True:
+        import torch
         return torch.empty(shape, dtype=dtype, device=like.device)
-    _check_tensor(what, out, (dtype,), shape, device)
+    _need(what, out, dtype, shape, device)
+    return out
+
+
+def _result(out, dtype, shape, device, like):
+    """The tensor ``out``, checked, or a new one where it is None."""
+    if out is None:
+        import torch
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _need("out", out, dtype, shape, device)
     return out
 
 
@@ -573,7 +593,7 @@ class USQLayer:
             raise ValueError("dtype must be f16 or bf16, y_dtype f16, bf16 or f32")
         if not isinstance(group, int) or group < 1:
             raise ValueError("group must be a positive int")
-        shape = tuple(codes.shape)
+        shape = tuple(getattr(codes, "shape", ()))
         if len(shape) != 2 or min(shape) < 1:
             raise ValueError(f"codes must be a matrix, got shape {shape}")
         self.C_out, self.K = shape[0], 2 * shape[1]
@@ -590,8 +610,8 @@ class USQLayer:
     def forward(self, x, out=None, stream=None):
         """Y [n, C_out] for the device tensor ``x`` [n, K]; returns ``out``."""
         n = _rows("x", x)
-        _check_tensor("x", x, (_torch_dtype(self.dtype),), (n, self.K), self.device)
-        out = _output("out", True if out is None else out, _torch_dtype(self.y_dtype), (n, self.C_out), self.device, x)
+        _need("x", x, _torch_dtype(self.dtype), (n, self.K), self.device)
+        out = _result(out, _torch_dtype(self.y_dtype), (n, self.C_out), self.device, x)
         st = stream if stream is not None else _current_stream(x.device.index)
         aq_usq_forward(self.handle, x.data_ptr(), out.data_ptr(), n, st)
         return out
@@ -602,8 +622,8 @@ class USQLayer:
         """dX [n, K] for the output gradient ``dy`` [n, C_out] (in ``dtype``); returns ``out``."""
         n = _rows("dy", dy)
         dt = _torch_dtype(self.dtype)
-        _check_tensor("dy", dy, (dt,), (n, self.C_out), self.device)
-        out = _output("out", True if out is None else out, dt, (n, self.K), self.device, dy)
+        _need("dy", dy, dt, (n, self.C_out), self.device)
+        out = _result(out, dt, (n, self.K), self.device, dy)
         st = stream if stream is not None else _current_stream(dy.device.index)
         aq_usq_input_grad(self.handle, dy.data_ptr(), out.data_ptr(), n, st)
         return out
@@ -639,22 +659,25 @@ class VocabLoss:
         self.handle = aq_loss_create(aq_loss_desc(vocab, features or 0, DTYPE_CODES[dtype], max_tokens))
 
     def _row_args(self, n, dloss, loss, like):
-        import torch
+        f32 = _torch_dtype("f32")
         if dloss is not None:
-            _check_tensor("dloss", dloss, (torch.float32,), (n,), self.device)
-        return _output("loss", True if loss is None else loss, torch.float32, (n,), self.device, like)
+            _need("dloss", dloss, f32, (n,), self.device)
+        if loss is None or loss is True:
+            import torch
+            return torch.empty(n, dtype=f32, device=like.device)
+        _need("loss", loss, f32, (n,), self.device)
+        return loss
 
     def cross_entropy(self, x, w, targets, dloss=None, loss=None, dx=None, dw=None, stream=None):
         """(loss [n], dX or None, dW or None) of the head ``w`` [vocab, features] on ``x`` [n, features] for the
         next tokens ``targets`` [n] (int64; negative: not counted), with ``dloss`` [n] (None: ones) the gradient
         with respect to each loss; see ``aq_loss_cross_entropy``."""
-        import torch
         if self.features is None:
             raise ValueError("created without features: distillation only")
         n, dt = _rows("x", x), _torch_dtype(self.dtype)
-        _check_tensor("x", x, (dt,), (n, self.features), self.device)
-        _check_tensor("w", w, (dt,), (self.vocab, self.features), self.device)
-        _check_tensor("targets", targets, (torch.int64,), (n,), self.device)
+        _need("x", x, dt, (n, self.features), self.device)
+        _need("w", w, dt, (self.vocab, self.features), self.device)
+        _need("targets", targets, _torch_dtype("i64"), (n,), self.device)
         loss = self._row_args(n, dloss, loss, x)
         dx = _output("dx", dx, dt, (n, self.features), self.device, x)
         dw = _output("dw", dw, dt, (self.vocab, self.features), self.device, x)
@@ -666,17 +689,18 @@ class VocabLoss:
     def distill(self, logits, ids, teacher, temperature: float = 1.0, dloss=None, loss=None, grad=None, stream=None):
         """(loss [n], gradient or None) of the student's ``logits`` [n, vocab] against the teacher's logits
         ``teacher`` [n, top] of the tokens ``ids`` [n, top] (int32; negative: empty); see ``aq_loss_distill``."""
-        import torch
         n, dt = _rows("logits", logits), _torch_dtype(self.dtype)
-        _check_tensor("logits", logits, (dt,), (n, self.vocab), self.device)
-        if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or ids.shape[1] < 1:
-            raise ValueError("ids must be a torch matrix with at least one column")
-        _check_tensor("ids", ids, (torch.int32,), (n, ids.shape[1]), self.device)
-        _check_tensor("teacher", teacher, (dt,), tuple(ids.shape), self.device)
+        _need("logits", logits, dt, (n, self.vocab), self.device)
+        _rows("ids", ids)
+        top = ids.shape[1]
+        if top < 1:
+            raise ValueError("ids must have at least one column")
+        _need("ids", ids, _torch_dtype("i32"), (n, top), self.device)
+        _need("teacher", teacher, dt, (n, top), self.device)
         loss = self._row_args(n, dloss, loss, logits)
         grad = _output("grad", grad, dt, (n, self.vocab), self.device, logits)
         st = stream if stream is not None else _current_stream(logits.device.index)
-        aq_loss_distill(self.handle, logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), ids.shape[1],
+        aq_loss_distill(self.handle, logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), top,
                         temperature, _ptr(dloss), loss.data_ptr(), _ptr(grad), n, st)
         return loss, grad
 

@@ -43,8 +43,10 @@ struct GemmOperands {
 };
 
 constexpr int kGemmChunk = 64;
-// a tile's 255 rows stay within 32-bit byte offsets
-constexpr int64_t kMaxPitch = 1 << 22;
+// a tile's 256 rows, of fp32 sums too, stay below byte offset kOutOfRange
+constexpr int64_t kMaxPitch = 1 << 21;
+// tiles of 128 x 128 a launch may hold (fewer than 2^32 threads, K splits included)
+constexpr int64_t kMaxTiles = 1 << 22;
 
 template <int DT>
 __device__ __forceinline__ floatx16 mfma_gemm(const u32x4& a, const u32x4& b, const floatx16& c) {
@@ -368,8 +370,8 @@ struct GemmPlan {
 
 // Shortest by a model of the calls: rounds of 256 big or 512 small tiles (one
 // or two a compute unit), a tile's fixed time and its time a chunk, and the
-// splits' sums.
-inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, bool may_split) {
+// splits' sums.  `cap`: bytes there are for them (0: no splits).
+inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, size_t cap) {
     const int chunks = (int)((K + kGemmChunk - 1) / kGemmChunk);
     GemmPlan best{true, 1, chunks};
     double best_us = 1e30;
@@ -377,8 +379,8 @@ inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, bool may_split) {
         const int64_t side = big ? 256 : 128, slots = big ? 256 : 512;
         const int64_t tiles = (M + side - 1) / side * ((N + side - 1) / side);
         const double fixed = big ? 12.0 : 7.0;
-        for (int s = 1; s <= (may_split ? std::min(chunks, 64) : 1); ++s) {
-            if (s > 1 && tiles * (s - 1) >= slots) break;
+        for (int s = 1; s <= std::min(chunks, 64); ++s) {
+            if (s > 1 && (tiles * (s - 1) >= slots || (size_t)s * M * N * 4 > cap)) break;
             const int cps = (chunks + s - 1) / s;
             if ((chunks + cps - 1) / cps != s) continue;
             const int64_t rounds = (tiles * s + slots - 1) / slots;
@@ -391,6 +393,17 @@ inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, bool may_split) {
         }
     }
     return best;
+}
+
+// Bytes of the split sums that calls of up to max_rows rows plan within `cap`.  Fewer rows of the same tiles never
+// split less (only the sums' time grows with the rows), so each step of 128 rows is bounded by its first row's splits.
+inline size_t gemm_split_bytes(int64_t max_rows, int64_t N, int64_t K, size_t cap) {
+    size_t need = 0;
+    for (int64_t lo = 1; lo <= max_rows && lo <= 128 * 512; lo += 128) {
+        const GemmPlan p = gemm_plan(lo, N, K, cap);
+        if (p.splits > 1) need = std::max(need, (size_t)p.splits * std::min(lo + 127, max_rows) * N * 4);
+    }
+    return std::min(need, cap);
 }
 
 template <int DT, int WM, int WN, int AM, int AN, bool TR, class Epi>

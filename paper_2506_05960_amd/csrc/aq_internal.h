@@ -49,6 +49,8 @@ void note_launch(hipStream_t st, const char* kernel, std::initializer_list<int> 
 // Record the message of a failing call (aq_last_error) and return its status.
 aq_status api_fail(aq_status status, const char* message);
 aq_status api_hip_fail(hipError_t e, const char* what);
+// Whether `st` is being captured into a graph (or cannot be asked because another stream is).
+bool capturing(hipStream_t st);
 
 // Raise a kernel's dynamic-LDS limit to at least `bytes` on the current
 // device (once per kernel and device; thread-safe).

@@ -179,6 +179,13 @@ namespace aq {
 aq_status api_fail(aq_status status, const char* message) { return fail(status, message); }
 aq_status api_hip_fail(hipError_t e, const char* what) { return hip_fail(e, what); }
 
+bool capturing(hipStream_t st) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+    (void)hipGetLastError();
+    return true;
+}
+
 }  // namespace aq
 
 namespace {

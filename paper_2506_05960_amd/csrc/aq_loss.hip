@@ -21,7 +21,8 @@ struct aq_loss {
     // gradient workspace, allocated by the first call that needs it
     uint16_t* d_dlt;       // [piece][tokens] logits' gradient of a piece
     uint16_t* d_xt;        // [features][tokens] inputs, transposed
-    float* d_dx;           // [max_tokens][features] input gradient of the pieces so far
+    float* d_dx;           // [split][tokens][features] input gradient of the pieces so far
+    size_t dx_bytes;
 };
 
 namespace aq {
@@ -540,7 +541,7 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     g.ldb = F;
     g.N = n;
     g.K = F;
-    GemmPlan p = gemm_plan(V, n, F, false);
+    GemmPlan p = gemm_plan(V, n, F, 0);
     e = p.big ? launch_gemm<DT, 2, 4, 4, 2, false>(g, p, StatsEpilogue<2, 4, 4, 2>{L->d_part, rs}, st)
               : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, StatsEpilogue<2, 2, 2, 2>{L->d_part, rs}, st);
     if (e != hipSuccess) return e;
@@ -551,13 +552,13 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     const Transpose tx = dW ? Transpose{X, L->d_xt, n, F, np, tiles_r, tiles_r * ((F + 63) / 64)} : Transpose{};
     prepare_kernel<<<(unsigned)tx.tiles + 1, 256, 0, st>>>(tx, rs, n);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const GemmPlan px = gemm_plan(n, F, std::min(V, piece), true);
+    const GemmPlan px = gemm_plan(n, F, std::min(V, piece), L->dx_bytes);
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
         const int rows = (int)std::min<int64_t>(piece, V - v0);
         const bool first = v0 == 0, last = v0 + piece >= V;
         g.A = W + v0 * F;
         g.M = rows;
-        p = gemm_plan(rows, n, F, false);
+        p = gemm_plan(rows, n, F, 0);
         e = p.big ? launch_gemm<DT, 2, 4, 4, 2, false>(g, p, GradEpilogue<DT, 2, 4, 4, 2>{L->d_dlt, piece, np, v0, rs}, st)
                   : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, GradEpilogue<DT, 2, 2, 2, 2>{L->d_dlt, piece, np, v0, rs}, st);
         if (e != hipSuccess) return e;
@@ -588,7 +589,7 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.M = rows;
             d.N = F;
             d.K = np;
-            e = launch_store_gemm<DT, false, STORE_OUT>(d, gemm_plan(rows, F, np, false),
+            e = launch_store_gemm<DT, false, STORE_OUT>(d, gemm_plan(rows, F, np, 0),
                                                         StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.scale + 1}, st);
             if (e != hipSuccess) return e;
         }
@@ -625,25 +626,23 @@ aq_status alloc(T** p, size_t bytes, const char* what) {
     return api_hip_fail(e, what);
 }
 
-// Bytes of the input gradient's fp32 sums: the most that a call of any token count takes (its plan has no
-// splits past 512 tiles, and changes at multiples of 128 tokens).
-size_t dx_bytes(const aq_loss* L) {
-    const int64_t mt = L->desc.max_tokens, F = L->desc.features;
-    size_t need = L->piece < L->desc.vocab ? (size_t)mt * F * 4 : 16;
-    for (int64_t n = 128; n < mt + 128 && n <= 128 * 512; n += 128) {
-        const int64_t t = std::min(n, mt);
-        const aq::GemmPlan p = aq::gemm_plan(t, F, std::min<int64_t>(L->desc.vocab, L->piece), true);
-        if (p.splits > 1) need = std::max(need, (size_t)p.splits * t * F * 4);
-    }
-    return need;
-}
+constexpr size_t kSplitBytes = size_t(64) << 20;   // most that a K split's sums of dX take
 
 // The gradients' workspace (the first call that asks for one allocates it).
-aq_status grad_workspace(aq_loss* L, bool dx, bool dw) {
+aq_status grad_workspace(aq_loss* L, bool dx, bool dw, void* stream) {
+    if (L->d_dlt && (!dx || L->d_dx) && (!dw || L->d_xt)) return AQ_OK;
+    if (aq::capturing(static_cast<hipStream_t>(stream)))
+        return api_fail(AQ_ERR_UNSUPPORTED, "the first call with a gradient allocates: not under graph capture");
     const size_t n = (size_t)(L->desc.max_tokens + 7) / 8 * 8, F = (size_t)L->desc.features, P = (size_t)L->piece;
     aq_status s = AQ_OK;
     s = alloc(&L->d_dlt, n * P * 2, "gradient workspace");
-    if (s == AQ_OK && dx) s = alloc(&L->d_dx, dx_bytes(L), "gradient workspace");
+    if (s == AQ_OK && dx && !L->d_dx) {
+        const int64_t mt = L->desc.max_tokens;
+        const size_t split = aq::gemm_split_bytes(mt, F, std::min<int64_t>(L->desc.vocab, L->piece), kSplitBytes);
+        const size_t bytes = std::max(split, L->piece < L->desc.vocab ? (size_t)mt * F * 4 : (size_t)16);
+        s = alloc(&L->d_dx, bytes, "gradient workspace");
+        if (s == AQ_OK) L->dx_bytes = bytes;
+    }
     if (s == AQ_OK && dw) s = alloc(&L->d_xt, n * F * 2, "gradient workspace");
     return s;
 }
@@ -678,7 +677,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
         return api_fail(AQ_ERR_UNSUPPORTED, "the cross entropy takes fp16 or bf16 inputs and head weights");
     if (desc->features % 8 != 0) return api_fail(AQ_ERR_UNSUPPORTED, "features must be a multiple of 8");
     if (desc->features > aq::kMaxPitch || (desc->features && desc->max_tokens > aq::kMaxPitch))
-        return api_fail(AQ_ERR_UNSUPPORTED, "features, or max_tokens of a cross entropy, above 2^22");
+        return api_fail(AQ_ERR_UNSUPPORTED, "features, or max_tokens of a cross entropy, above 2^21");
     int ndev = 0;
     hipError_t e = hipGetDeviceCount(&ndev);
     if (e != hipSuccess || ndev < 1) return api_fail(AQ_ERR_DEVICE, "no HIP device available");
@@ -692,7 +691,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
     }
     if (desc->features) {
         // a piece's gradient takes at most 128 MiB, its head rows too
-        const int64_t most = std::min(aq::kMaxPitch / 2, std::max<int64_t>(256, (int64_t(64) << 20) / std::max<int64_t>(
+        const int64_t most = std::min(aq::kMaxPitch, std::max<int64_t>(256, (int64_t(64) << 20) / std::max<int64_t>(
                                                                               desc->max_tokens, desc->features)));
         const int64_t pieces = (desc->vocab + most - 1) / most;
         L->piece = (int)(((desc->vocab + pieces - 1) / pieces + 255) / 256 * 256);
@@ -722,8 +721,11 @@ aq_status aq_loss_cross_entropy(aq_loss* L, const void* X, const void* W, const 
         return api_fail(AQ_ERR_INVALID_ARGUMENT, "dloss and loss must be 4-byte aligned");
     aq_status s = check_call(L, n);
     if (s != AQ_OK) return s;
+    const int64_t F = L->desc.features, tiles_n = (n + 127) / 128;
+    if (tiles_n * ((L->desc.vocab + 127) / 128) > aq::kMaxTiles || tiles_n * ((F + 127) / 128) > aq::kMaxTiles)
+        return api_fail(AQ_ERR_UNSUPPORTED, "too many tokens times vocabulary or features for one call");
     if (dX || dW) {
-        s = grad_workspace(L, dX != nullptr, dW != nullptr);
+        s = grad_workspace(L, dX != nullptr, dW != nullptr, stream);
         if (s != AQ_OK) return s;
     }
     const int64_t mt = L->desc.max_tokens;

@@ -42,6 +42,7 @@ struct aq_usq {
     // input gradient, allocated by its first call
     uint16_t* d_wt;        // [slab][Cp] decoded weights of a slab of inputs, transposed
     float* d_dsum;         // a K split's partial sums
+    size_t dsum_bytes, part_bytes;
     uint16_t* d_dy;        // [max_tokens][Cp] output gradient with rows of whole 16-byte groups (C_out % 8 != 0)
     int slab, cp;
 };
@@ -370,26 +371,26 @@ template <int DT>
 __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
     // eight lanes a group, 16-byte loads
     const int gp = a.sum_groups;
-    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
     const int part = threadIdx.x & 7;
-    if (id >= (int64_t)a.n * gp) return;
-    const int64_t t = id / gp;
-    const int j = (int)(id - t * gp);
-    float s = 0.0f;
-    for (int k = j * group + 8 * part; k < min((j + 1) * group, a.K); k += 64) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(a.X + t * a.K + k);
+    for (int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3; id < (int64_t)a.n * gp; id += (int64_t)gridDim.x * 32) {
+        const int64_t t = id / gp;
+        const int j = (int)(id - t * gp);
+        float s = 0.0f;
+        for (int k = j * group + 8 * part; k < min((j + 1) * group, a.K); k += 64) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(a.X + t * a.K + k);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += widen16<DT>((uint16_t)v[e]) + widen16<DT>((uint16_t)(v[e] >> 16));
+            for (int e = 0; e < 4; ++e) s += widen16<DT>((uint16_t)v[e]) + widen16<DT>((uint16_t)(v[e] >> 16));
+        }
+        s += __shfl_xor(s, 1);
+        s += __shfl_xor(s, 2);
+        s += __shfl_xor(s, 4);
+        if (part != 0) continue;
+        const uint32_t h = f32_to_bf16(s);
+        const float r1 = s - bf16_to_f32((uint16_t)h);
+        const uint32_t m = f32_to_bf16(r1);
+        const uint32_t l = f32_to_bf16(r1 - bf16_to_f32((uint16_t)m));
+        reinterpret_cast<u32x4*>(a.sums)[(int64_t)j * a.n + t] = u32x4{h | m << 16, l | h << 16, m | l << 16, 0u};
     }
-    s += __shfl_xor(s, 1);
-    s += __shfl_xor(s, 2);
-    s += __shfl_xor(s, 4);
-    if (part != 0) return;
-    const uint32_t h = f32_to_bf16(s);
-    const float r1 = s - bf16_to_f32((uint16_t)h);
-    const uint32_t m = f32_to_bf16(r1);
-    const uint32_t l = f32_to_bf16(r1 - bf16_to_f32((uint16_t)m));
-    reinterpret_cast<u32x4*>(a.sums)[(int64_t)j * a.n + t] = u32x4{h | m << 16, l | h << 16, m | l << 16, 0u};
 }
 
 // A 2 x 2 grid of waves on a (64 AM) x (64 AN) tile of tokens x output rows;
@@ -664,12 +665,13 @@ struct UsqPlan {
 // K splits of a call, shortest by a model fitted to it: a workgroup's fixed
 // time, 1.3 us a chunk alone on its compute unit and 2.3 with a second one,
 // and the partial sums written and read back (256 tokens, 4096 -> 4096: four
-// splits 30 us, eight 36).
-UsqPlan usq_plan(int64_t n, int C_out, int nchunk) {
+// splits 30 us, eight 36).  `cap`: bytes there are for the sums.
+UsqPlan usq_plan(int64_t n, int C_out, int nchunk, size_t cap) {
     const int64_t tiles = (n + 127) / 128 * ((C_out + 127) / 128);
     UsqPlan best{(int)tiles, 1, nchunk};
     double best_us = 1e30;
     for (int s = 1; s <= std::max(1, nchunk / 2) && tiles * s <= std::max<int64_t>(tiles, 512); ++s) {
+        if (s > 1 && (size_t)s * n * C_out * 4 > cap) break;
         const int cps = (nchunk + s - 1) / s;
         if ((nchunk + cps - 1) / cps != s) continue;
         const int64_t wgs = tiles * s;
@@ -695,10 +697,10 @@ hipError_t launch_usq_gemm(const UsqArgs& a, int grid, hipStream_t st) {
 }
 
 template <int DT, int SG>
-hipError_t launch_many(UsqArgs a, int group, float* part, hipStream_t st) {
-    const UsqPlan p = usq_plan(a.n, a.C_out, a.nchunk);
-    const int64_t sums = (int64_t)a.n * a.sum_groups;
-    usq_sums_kernel<DT><<<(unsigned)((sums * 8 + 255) / 256), 256, 0, st>>>(a, group);
+hipError_t launch_many(UsqArgs a, int group, float* part, size_t part_bytes, hipStream_t st) {
+    const UsqPlan p = usq_plan(a.n, a.C_out, a.nchunk, part_bytes);
+    const int64_t blocks = ((int64_t)a.n * a.sum_groups * 8 + 255) / 256;
+    usq_sums_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), 256, 0, st>>>(a, group);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.cps = p.cps;
@@ -712,12 +714,12 @@ hipError_t launch_many(UsqArgs a, int group, float* part, hipStream_t st) {
 }
 
 template <int DT>
-hipError_t launch_usq_forward(const UsqArgs& a, int group, float* part, hipStream_t st) {
+hipError_t launch_usq_forward(const UsqArgs& a, int group, float* part, size_t pb, hipStream_t st) {
     if (a.n <= kFewTokens)
         return group == 32 ? launch_few<DT, 1>(a, st) : group == 64 ? launch_few<DT, 2>(a, st) : launch_few<DT, 4>(a, st);
-    return group == 32   ? launch_many<DT, 2>(a, group, part, st)
-           : group == 64 ? launch_many<DT, 4>(a, group, part, st)
-                         : launch_many<DT, 8>(a, group, part, st);
+    return group == 32   ? launch_many<DT, 2>(a, group, part, pb, st)
+           : group == 64 ? launch_many<DT, 4>(a, group, part, pb, st)
+                         : launch_many<DT, 8>(a, group, part, pb, st);
 }
 
 // ---- input gradient ----
@@ -793,7 +795,7 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
             a, L->desc.group, k0 / 128, L->d_wt, cp);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         g.N = cols;
-        const GemmPlan p = gemm_plan(n, cols, cp, true);
+        const GemmPlan p = gemm_plan(n, cols, cp, L->dsum_bytes);
         const StoreArgs<DT> s{dX + k0, L->d_dsum, K, nullptr};
         e = p.splits > 1 ? launch_store_gemm<DT, false, STORE_SUM>(g, p, s, st)
                          : launch_store_gemm<DT, false, STORE_OUT>(g, p, s, st);
@@ -829,6 +831,9 @@ aq_status alloc(T** p, size_t bytes, const char* what) {
 
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
+constexpr size_t kPartBytes = size_t(32) << 20;    // most that the forward's K splits take
+constexpr size_t kSplitBytes = size_t(64) << 20;   // and the input gradient's
+
 // Weights into the device layout, through a staging buffer that is freed again.
 aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t* zeros) {
     const aq_usq_desc& d = L->desc;
@@ -843,14 +848,15 @@ aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t
     if (s == AQ_OK && d.max_tokens > aq::kFewTokens) {
         L->sum_groups = G;
         s = alloc(&L->d_sums, (size_t)d.max_tokens * L->sum_groups * 16, "group sums");
-        // the plan's token counts change only at multiples of 128; a split holds at most 512 tiles
+        // (fewer tokens of the same tiles never split less: each step of 128 is bounded by its first token's splits)
         size_t need = 0;
-        for (int64_t n = 128; n < d.max_tokens + 128 && n <= 128 * 512; n += 128) {
-            const int64_t t = std::min(n, d.max_tokens);
-            const aq::UsqPlan p = aq::usq_plan(t, d.out_features, L->nchunk);
-            if (p.splits > 1) need = std::max(need, (size_t)p.splits * t * d.out_features * 4);
+        for (int64_t lo = 1; lo <= d.max_tokens && lo <= 128 * 512; lo += 128) {
+            const aq::UsqPlan p = aq::usq_plan(lo, d.out_features, L->nchunk, kPartBytes);
+            if (p.splits > 1) need = std::max(need, (size_t)p.splits * std::min(lo + 127, d.max_tokens) * d.out_features * 4);
         }
+        need = std::min(need, kPartBytes);
         if (s == AQ_OK && need) s = alloc(&L->d_part, need, "partial sums");
+        if (s == AQ_OK) L->part_bytes = need;
     }
     uint8_t* tmp = nullptr;
     if (s == AQ_OK) s = alloc(&tmp, std::max(code_bytes, group_count * 2), "staging buffer");
@@ -894,23 +900,10 @@ aq_status check_call(const aq_usq* L, const void* in, const void* out, int64_t n
     const hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return api_hip_fail(e, "hipGetDevice");
     if (dev != L->device) return api_fail(AQ_ERR_INVALID_ARGUMENT, "layer created on another device");
+    const int64_t wide = std::max(L->desc.in_features, L->desc.out_features);
+    if ((n + 127) / 128 * ((wide + 127) / 128) > aq::kMaxTiles)
+        return api_fail(AQ_ERR_UNSUPPORTED, "too many tokens times features for one call");
     return AQ_OK;
-}
-
-// Bytes of the input gradient's split sums: the most that a call of any token count takes (its plan has no
-// splits past 512 tiles, and changes at multiples of 128 tokens).
-size_t dsum_bytes(const aq_usq* L) {
-    const int64_t mt = L->desc.max_tokens;
-    const int tail = L->desc.in_features % L->slab;
-    size_t need = 16;
-    for (int64_t n = 128; n < mt + 128 && n <= 128 * 512; n += 128)
-        for (const int64_t cols : {std::min(L->slab, L->desc.in_features), tail}) {
-            if (!cols) continue;
-            const int64_t t = std::min(n, mt);
-            const aq::GemmPlan p = aq::gemm_plan(t, cols, L->cp, true);
-            if (p.splits > 1) need = std::max(need, (size_t)p.splits * t * cols * 4);
-        }
-    return need;
 }
 
 aq::UsqArgs make_args(const aq_usq* L, const void* X, void* Y, int64_t n) {
@@ -940,7 +933,7 @@ aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* 
     if (d.group != 32 && d.group != 64 && d.group % 128 != 0)
         return api_fail(AQ_ERR_UNSUPPORTED, "group must be 32, 64 or a multiple of 128");
     if (d.in_features > aq::kMaxPitch || d.out_features > aq::kMaxPitch || d.max_tokens > (1 << 24))
-        return api_fail(AQ_ERR_UNSUPPORTED, "features above 2^22 or max_tokens above 2^24");
+        return api_fail(AQ_ERR_UNSUPPORTED, "features above 2^21 or max_tokens above 2^24");
     if (zeros) {
         const int64_t count = (int64_t)d.out_features * ((d.in_features + (int64_t)d.group - 1) / d.group);
         for (int64_t i = 0; i < count; ++i)
@@ -973,8 +966,8 @@ aq_status aq_usq_forward(aq_usq* L, const void* X, void* Y, int64_t n, void* str
     if (s != AQ_OK) return s;
     const aq::UsqArgs a = make_args(L, X, Y, n);
     const auto st = static_cast<hipStream_t>(stream);
-    const hipError_t e = L->desc.dtype == AQ_F16 ? aq::launch_usq_forward<AQ_F16>(a, L->desc.group, L->d_part, st)
-                                                 : aq::launch_usq_forward<AQ_BF16>(a, L->desc.group, L->d_part, st);
+    const hipError_t e = L->desc.dtype == AQ_F16 ? aq::launch_usq_forward<AQ_F16>(a, L->desc.group, L->d_part, L->part_bytes, st)
+                                                 : aq::launch_usq_forward<AQ_BF16>(a, L->desc.group, L->d_part, L->part_bytes, st);
     return e == hipSuccess ? AQ_OK : api_hip_fail(e, "forward launch");
 }
 
@@ -987,8 +980,16 @@ aq_status aq_usq_input_grad(aq_usq* L, const void* dY, void* dX, int64_t n, void
         const int64_t most = std::max<int64_t>(128, (int64_t(16) << 20) / L->cp / 128 * 128);   // 32 MiB
         L->slab = (int)std::min<int64_t>(most, (int64_t)L->nchunk * 128);
     }
+    if ((!L->d_wt || !L->d_dsum || (C % 8 != 0 && !L->d_dy)) && aq::capturing(static_cast<hipStream_t>(stream)))
+        return api_fail(AQ_ERR_UNSUPPORTED, "the first input gradient allocates: not under graph capture");
     s = alloc(&L->d_wt, (size_t)L->slab * L->cp * 2, "gradient workspace");
-    if (s == AQ_OK) s = alloc(&L->d_dsum, dsum_bytes(L), "gradient workspace");
+    if (s == AQ_OK && !L->d_dsum) {
+        const int cols = std::min(L->slab, L->desc.in_features), tail = L->desc.in_features % L->slab;
+        size_t bytes = std::max<size_t>(16, aq::gemm_split_bytes(L->desc.max_tokens, cols, L->cp, kSplitBytes));
+        if (tail) bytes = std::max(bytes, aq::gemm_split_bytes(L->desc.max_tokens, tail, L->cp, kSplitBytes));
+        s = alloc(&L->d_dsum, bytes, "gradient workspace");
+        if (s == AQ_OK) L->dsum_bytes = bytes;
+    }
     if (s == AQ_OK && C % 8 != 0) s = alloc(&L->d_dy, (size_t)L->desc.max_tokens * L->cp * 2, "gradient workspace");
     if (s != AQ_OK) return s;
     const aq::UsqArgs a = make_args(L, nullptr, nullptr, n);

@@ -314,6 +314,33 @@ def test_cross_entropy_gradient_matches_differences():
     assert float((slope - dx[0].double()).abs().max()) <= bound
 
 
+def test_first_gradient_under_capture_is_refused():
+    import paper_2506_05960_amd as P
+    n, F, V = 9, 16, 40
+    x, w, targets, dloss = ce_inputs(n, F, V, "bf16", 3)
+    L = losses(V, F, "bf16", n)
+    loss, dx = torch.empty(n, device="cuda"), torch.empty_like(x)
+    want, _, _ = L.cross_entropy(x, w, targets, dloss)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(P.AQError, match="capture"):
+            L.cross_entropy(x, w, targets, dloss, loss=loss, dx=dx)
+        L.cross_entropy(x, w, targets, dloss, loss=loss)      # the loss alone needs nothing more
+    loss.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(loss, want)
+
+
+@pytest.mark.parametrize("n", [1, 40, 65, 130, 257, 700])
+def test_token_counts_below_the_most(n):
+    """Handles made for many tokens serve fewer: their plans differ, their workspace holds each."""
+    F, V = 136, 3000
+    x, w, targets, dloss = ce_inputs(n, F, V, "f16", n)
+    L = losses(V, F, "f16", 700)
+    check_ce(x, w, targets, dloss, "f16", *L.cross_entropy(x, w, targets, dloss, dx=True, dw=True))
+
+
 def test_losses_on_another_stream_and_in_graphs():
     n, F, V = 90, 72, 1031
     L = losses(V, F, "bf16", n)

@@ -191,6 +191,22 @@ def test_another_stream_and_graph_replays():
         assert torch.equal(y, want[r % 3][0]) and torch.equal(dx, want[r % 3][1])
 
 
+def test_first_gradient_under_capture_is_refused():
+    import paper_2506_05960_amd as P
+    codes, scales, z, _, _ = make(128, 24, 32, "f16", False)
+    lay = layer_of(codes, scales, z, 32, "f16", "f16", 4)
+    dy, dx, t = torch.ones(4, 24, device="cuda").half(), torch.empty(4, 128, device="cuda").half(), torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(P.AQError, match="capture"):
+            lay.input_grad(dy, out=dx)
+        t += 1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(t.sum()) == 4
+    lay.input_grad(dy, out=dx)               # outside: allocates and runs
+
+
 def test_numpy_arrays_and_raw_bf16_bits():
     codes, scales, z, _, _ = make(128, 24, 32, "bf16", True)
     x = torch.randn(3, 128, device="cuda").bfloat16()

@@ -41,8 +41,8 @@ def _create_usq(no=None, zeros=None, **change):
     (dict(group=96), A.AQ_ERR_UNSUPPORTED, "group"),
     (dict(group=192), A.AQ_ERR_UNSUPPORTED, "group"),
     (dict(max_tokens=1 << 40), A.AQ_ERR_UNSUPPORTED, "2^24"),
-    (dict(out_features=(1 << 22) + 1), A.AQ_ERR_UNSUPPORTED, "2^22"),
-    (dict(in_features=(1 << 22) + 8), A.AQ_ERR_UNSUPPORTED, "2^22"),
+    (dict(out_features=(1 << 21) + 1), A.AQ_ERR_UNSUPPORTED, "2^21"),
+    (dict(in_features=(1 << 21) + 8), A.AQ_ERR_UNSUPPORTED, "2^21"),
 ])
 def test_usq_create_refuses(change, status, text):
     st, h, msg = _create_usq(**change)
@@ -76,8 +76,8 @@ def _create_loss(**change):
     (dict(features=60), A.AQ_ERR_UNSUPPORTED, "multiple of 8"),
     (dict(vocab=(1 << 30) + 1), A.AQ_ERR_UNSUPPORTED, "vocab"),
     (dict(max_tokens=(1 << 24) + 1), A.AQ_ERR_UNSUPPORTED, "max_tokens"),
-    (dict(features=(1 << 22) + 8), A.AQ_ERR_UNSUPPORTED, "features"),
-    (dict(max_tokens=(1 << 22) + 1), A.AQ_ERR_UNSUPPORTED, "max_tokens"),
+    (dict(features=(1 << 21) + 8), A.AQ_ERR_UNSUPPORTED, "features"),
+    (dict(max_tokens=(1 << 21) + 1), A.AQ_ERR_UNSUPPORTED, "max_tokens"),
 ])
 def test_loss_create_refuses(change, status, text):
     st, h, msg = _create_loss(**change)
@@ -190,7 +190,8 @@ def test_loss_calls_refuse(so):
     assert left == 0
 
 
-@pytest.mark.parametrize("n,features,vocab,top", [(1, 8, 1, 1), (70000, 64, 1000, 5), (3, 8, 3000000, 1024), (1 << 22, 8, 9, 1)])
+@pytest.mark.parametrize("n,features,vocab,top", [(1, 8, 1, 1), (70000, 64, 1000, 5), (3, 8, 3000000, 1024), (1 << 21, 8, 9, 1),
+                                                    (257, 1 << 21, 300, 3)])
 def test_loss_launches_stay_in_limits(so, n, features, vocab, top):
     assert host_device.in_child(so, "test_usq_losses_host", "launch_limits", n, features, vocab, top) == [0, 0]
 
