@@ -423,23 +423,27 @@ struct GradEpilogue {
     }
 };
 
-// Maximum, sum, loss and row weight of every token from its tiles' parts:
-// sixteen tokens a workgroup, sixteen threads a token.
+// Maximum, sum, loss and row weight of every token from its tiles' parts: TOK
+// tokens a workgroup, 256 / TOK threads a token (sixteen tokens make whole
+// lines; four are sooner done where there are few).
+template <int TOK>
 __global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* part, int tiles, int n, int64_t V) {
-    __shared__ float2 red[16][16];
-    const int tok = threadIdx.x & 15, p = threadIdx.x >> 4;
-    const int t = blockIdx.x * 16 + tok;
+    constexpr int kParts = 256 / TOK;
+    __shared__ float2 red[kParts][TOK];
+    const int tok = threadIdx.x % TOK, p = threadIdx.x / TOK;
+    const int t = blockIdx.x * TOK + tok;
     float m = -INFINITY, s = 0.0f;
     if (t < n)
-        for (int i = p; i < tiles; i += 16) {
+#pragma unroll 4
+        for (int i = p; i < tiles; i += kParts) {
             const float2 v = part[(int64_t)i * n + t];
             merge(m, s, v.x, v.y, kLog2e);
         }
     red[p][tok] = make_float2(m, s);
     __syncthreads();
     if (p != 0 || t >= n) return;
-#pragma unroll
-    for (int w = 1; w < 16; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
+#pragma unroll 8
+    for (int w = 1; w < kParts; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
     const int64_t target = rs.targets[t];
     float ls = __builtin_amdgcn_logf(s);
     float w = rs.dloss ? rs.dloss[t] : 1.0f;
@@ -546,7 +550,8 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
               : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, StatsEpilogue<2, 2, 2, 2>{L->d_part, rs}, st);
     if (e != hipSuccess) return e;
     const int side = p.big ? 256 : 128;
-    join_kernel<<<(unsigned)((n + 15) / 16), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
+    if (n > 64) join_kernel<16><<<(unsigned)((n + 15) / 16), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
+    else join_kernel<4><<<(unsigned)((n + 3) / 4), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
     if ((e = hipGetLastError()) != hipSuccess || (!dX && !dW)) return e;
     const int tiles_r = (np + 63) / 64;
     const Transpose tx = dW ? Transpose{X, L->d_xt, n, F, np, tiles_r, tiles_r * ((F + 63) / 64)} : Transpose{};

@@ -662,12 +662,14 @@ struct UsqPlan {
     int tiles, splits, cps;
 };
 
-// K splits of a call, shortest by a model fitted to it: a workgroup's fixed
-// time, 1.3 us a chunk alone on its compute unit and 2.3 with a second one,
-// and the partial sums written and read back (256 tokens, 4096 -> 4096: four
-// splits 30 us, eight 36).  `cap`: bytes there are for the sums.
-UsqPlan usq_plan(int64_t n, int C_out, int nchunk, size_t cap) {
+// K splits of a call, shortest by a model fitted to measured ones (4096 -> 4096, us with 1 / 2 / 3 / 4 / 8 splits:
+// 128 tokens 48 / 31 / 26 / 26 / 28, 256 tokens 49 / 35 / 31 / 34 / 37, 1024 tokens 59 / 54 / - / - / -; 16384 ->
+// 4096, 128 tokens 194 / 103 / 73 / 58 / 39): a workgroup's fixed time, its time a chunk alone on its compute unit or
+// with a second one (more of it the smaller the groups), and the partial sums written and read back.  `cap`: bytes
+// there are for them.
+UsqPlan usq_plan(int64_t n, int C_out, int nchunk, int group, size_t cap) {
     const int64_t tiles = (n + 127) / 128 * ((C_out + 127) / 128);
+    const double small = group == 32 ? 1.6 : group == 64 ? 1.2 : 1.0;
     UsqPlan best{(int)tiles, 1, nchunk};
     double best_us = 1e30;
     for (int s = 1; s <= std::max(1, nchunk / 2) && tiles * s <= std::max<int64_t>(tiles, 512); ++s) {
@@ -675,8 +677,9 @@ UsqPlan usq_plan(int64_t n, int C_out, int nchunk, size_t cap) {
         const int cps = (nchunk + s - 1) / s;
         if ((nchunk + cps - 1) / cps != s) continue;
         const int64_t wgs = tiles * s;
-        const double work = wgs <= 256 ? 7.0 + 1.3 * cps : (double)((wgs + 511) / 512) * (7.0 + 2.3 * cps);
-        const double us = work + (s > 1 ? 4.5 + 2e-6 * s * n * C_out : 0.0);
+        const double work = wgs <= 256 ? 5.0 + (1.4 + wgs * 0.001) * small * cps
+                                       : (double)((wgs + 511) / 512) * (5.0 + 2.3 * small * cps);
+        const double us = work + (s > 1 ? s * (1.0 + 1.3e-6 * n * C_out) : 0.0);
         if (us < best_us) {
             best_us = us;
             best.splits = s;
@@ -698,7 +701,7 @@ hipError_t launch_usq_gemm(const UsqArgs& a, int grid, hipStream_t st) {
 
 template <int DT, int SG>
 hipError_t launch_many(UsqArgs a, int group, float* part, size_t part_bytes, hipStream_t st) {
-    const UsqPlan p = usq_plan(a.n, a.C_out, a.nchunk, part_bytes);
+    const UsqPlan p = usq_plan(a.n, a.C_out, a.nchunk, group, part_bytes);
     const int64_t blocks = ((int64_t)a.n * a.sum_groups * 8 + 255) / 256;
     usq_sums_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), 256, 0, st>>>(a, group);
     hipError_t e = hipGetLastError();
@@ -851,7 +854,7 @@ aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t
         // (fewer tokens of the same tiles never split less: each step of 128 is bounded by its first token's splits)
         size_t need = 0;
         for (int64_t lo = 1; lo <= d.max_tokens && lo <= 128 * 512; lo += 128) {
-            const aq::UsqPlan p = aq::usq_plan(lo, d.out_features, L->nchunk, kPartBytes);
+            const aq::UsqPlan p = aq::usq_plan(lo, d.out_features, L->nchunk, d.group, kPartBytes);
             if (p.splits > 1) need = std::max(need, (size_t)p.splits * std::min(lo + 127, d.max_tokens) * d.out_features * 4);
         }
         need = std::min(need, kPartBytes);
