@@ -466,7 +466,8 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
  *   n        1 <= n <= max_tokens
  * Sums are fp32; dz is rounded once to desc->dtype before the products (scaled
  * so that the largest |dloss| lies just below 2^15).
- * dX and dW must overlap nothing else.
+ * dX, dW and loss must overlap nothing else (a loss that overlaps dloss is
+ * refused).
  * The first call with dX or with dW allocates its workspace (synchronous;
  * refused with AQ_ERR_UNSUPPORTED on a stream under graph capture): 2 bytes
  * per token and vocabulary row of a piece (at most 128 MiB, or 256 rows), for
@@ -493,7 +494,7 @@ aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void*
  *   teacher  device [n][top] in desc->dtype, the teacher's logits
  *   top      1 <= top <= 1024
  *   dloss    device [n] fp32; NULL: ones
- *   loss     device [n] fp32, overwritten
+ *   loss     device [n] fp32, overwritten; must overlap nothing else
  *   dlogits  device [n][vocab] in desc->dtype, overwritten; 16-byte aligned;
  *            may be `logits` itself; NULL: not computed
  *   n        1 <= n <= max_tokens

@@ -423,44 +423,6 @@ struct GradEpilogue {
     }
 };
 
-// Maximum, sum, loss and row weight of every token from its tiles' parts: TOK
-// tokens a workgroup, 256 / TOK threads a token (sixteen tokens make whole
-// lines; four are sooner done where there are few).
-template <int TOK>
-__global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* part, int tiles, int n, int64_t V) {
-    constexpr int kParts = 256 / TOK;
-    __shared__ float2 red[kParts][TOK];
-    const int tok = threadIdx.x % TOK, p = threadIdx.x / TOK;
-    const int t = blockIdx.x * TOK + tok;
-    float m = -INFINITY, s = 0.0f;
-    if (t < n)
-#pragma unroll 4
-        for (int i = p; i < tiles; i += kParts) {
-            const float2 v = part[(int64_t)i * n + t];
-            merge(m, s, v.x, v.y, kLog2e);
-        }
-    red[p][tok] = make_float2(m, s);
-    __syncthreads();
-    if (p != 0 || t >= n) return;
-#pragma unroll 8
-    for (int w = 1; w < kParts; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
-    const int64_t target = rs.targets[t];
-    float ls = __builtin_amdgcn_logf(s);
-    float w = rs.dloss ? rs.dloss[t] : 1.0f;
-    float l = 0.0f;
-    if (target < 0) {
-        w = 0.0f;
-    } else if (target >= V) {
-        ls = l = NAN;
-    } else {
-        l = (m - rs.zt[t]) + kLn2 * ls;
-    }
-    rs.loss[t] = l;
-    rs.top[t] = m;
-    rs.ls[t] = ls;
-    rs.w[t] = w;
-}
-
 // Factor that takes the largest row weight just below 2^15.  Stored gradients of an fp16 model then keep fp16's
 // relative precision whatever the weights' size, and the target's entry, (p - 1) times the weight and often the
 // largest of its row, lies where the type's steps are finest relative to it (equal weights: half the error of the
@@ -520,11 +482,62 @@ __device__ __forceinline__ void transpose_tile(const Transpose& a, int tile_id, 
     }
 }
 
-// What the gradient's products need beside the logits, in one launch: the scale, and for dW the transposed inputs
-// (rows that do not count left out: zeros times what they hold may not reach dW).
-__global__ void __launch_bounds__(256) prepare_kernel(Transpose x, RowState rs, int n) {
-    if ((int)blockIdx.x < x.tiles) transpose_tile(x, (int)blockIdx.x, rs);
+// Maximum, sum, loss and row weight of every token from its tiles' parts: TOK
+// tokens a workgroup, 256 / TOK threads a token (sixteen tokens make whole
+// lines; four are sooner done where there are few).
+template <int TOK>
+__device__ __forceinline__ void join_tokens(const RowState& rs, const float2* part, int tiles, int n, int64_t V) {
+    constexpr int kParts = 256 / TOK;
+    __shared__ float2 red[kParts][TOK];
+    const int tok = threadIdx.x % TOK, p = threadIdx.x / TOK;
+    const int t = blockIdx.x * TOK + tok;
+    float m = -INFINITY, s = 0.0f;
+    if (t < n)
+#pragma unroll 4
+        for (int i = p; i < tiles; i += kParts) {
+            const float2 v = part[(int64_t)i * n + t];
+            merge(m, s, v.x, v.y, kLog2e);
+        }
+    red[p][tok] = make_float2(m, s);
+    __syncthreads();
+    if (p != 0 || t >= n) return;
+#pragma unroll 8
+    for (int w = 1; w < kParts; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
+    const int64_t target = rs.targets[t];
+    float ls = __builtin_amdgcn_logf(s);
+    float w = rs.dloss ? rs.dloss[t] : 1.0f;
+    float l = 0.0f;
+    if (target < 0) {
+        w = 0.0f;
+    } else if (target >= V) {
+        ls = l = NAN;
+    } else {
+        l = (m - rs.zt[t]) + kLn2 * ls;
+    }
+    rs.loss[t] = l;
+    rs.top[t] = m;
+    rs.ls[t] = ls;
+    rs.w[t] = w;
+}
+
+// Between the statistics and the gradient, in one launch: the tokens' joins, and what the gradient's products need
+// beside the logits: for dW the transposed inputs (rows that do not count left out: zeros times what they hold may not
+// reach dW), and the scale.
+template <int TOK>
+__global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* part, int tiles, int n, int64_t V,
+                                                   Transpose x) {
+    const int joins = (n + TOK - 1) / TOK, b = (int)blockIdx.x;
+    if (b < joins) join_tokens<TOK>(rs, part, tiles, n, V);
+    else if (b < joins + x.tiles) transpose_tile(x, b - joins, rs);
     else find_scale(rs, n);
+}
+
+template <int TOK>
+hipError_t launch_join(const RowState& rs, const float2* part, int tiles, int n, int64_t V, const Transpose& x, bool grad,
+                       hipStream_t st) {
+    const unsigned blocks = (unsigned)((n + TOK - 1) / TOK + (grad ? x.tiles + 1 : 0));
+    join_kernel<TOK><<<blocks, 256, 0, st>>>(rs, part, tiles, n, V, x);
+    return hipGetLastError();
 }
 
 int round_up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
@@ -550,13 +563,11 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
               : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, StatsEpilogue<2, 2, 2, 2>{L->d_part, rs}, st);
     if (e != hipSuccess) return e;
     const int side = p.big ? 256 : 128;
-    if (n > 64) join_kernel<16><<<(unsigned)((n + 15) / 16), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
-    else join_kernel<4><<<(unsigned)((n + 3) / 4), 256, 0, st>>>(rs, L->d_part, (V + side - 1) / side, n, V);
-    if ((e = hipGetLastError()) != hipSuccess || (!dX && !dW)) return e;
     const int tiles_r = (np + 63) / 64;
     const Transpose tx = dW ? Transpose{X, L->d_xt, n, F, np, tiles_r, tiles_r * ((F + 63) / 64)} : Transpose{};
-    prepare_kernel<<<(unsigned)tx.tiles + 1, 256, 0, st>>>(tx, rs, n);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = n > 64 ? launch_join<16>(rs, L->d_part, (V + side - 1) / side, n, V, tx, dX || dW, st)
+               : launch_join<4>(rs, L->d_part, (V + side - 1) / side, n, V, tx, dX || dW, st);
+    if (e != hipSuccess || (!dX && !dW)) return e;
     const GemmPlan px = gemm_plan(n, F, std::min(V, piece), L->dx_bytes);
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
         const int rows = (int)std::min<int64_t>(piece, V - v0);
@@ -652,6 +663,9 @@ aq_status grad_workspace(aq_loss* L, bool dx, bool dw, void* stream) {
     return s;
 }
 
+// Joined rows' losses are written while other workgroups still read dloss.
+bool overlaps(const float* a, const float* b, int64_t n) { return a && b && a < b + n && b < a + n; }
+
 bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 aq_status check_call(const aq_loss* L, int64_t n) {
@@ -726,6 +740,7 @@ aq_status aq_loss_cross_entropy(aq_loss* L, const void* X, const void* W, const 
         return api_fail(AQ_ERR_INVALID_ARGUMENT, "dloss and loss must be 4-byte aligned");
     aq_status s = check_call(L, n);
     if (s != AQ_OK) return s;
+    if (overlaps(loss, dloss, n)) return api_fail(AQ_ERR_INVALID_ARGUMENT, "loss overlaps dloss");
     const int64_t F = L->desc.features, tiles_n = (n + 127) / 128;
     if (tiles_n * ((L->desc.vocab + 127) / 128) > aq::kMaxTiles || tiles_n * ((F + 127) / 128) > aq::kMaxTiles)
         return api_fail(AQ_ERR_UNSUPPORTED, "too many tokens times vocabulary or features for one call");

@@ -120,7 +120,7 @@ def loss_calls():
     _, plain, _ = _create_loss(features=0, dtype=A.AQ_F32)
     P = 4096
 
-    def ce(X=P, W=P, targets=P, dloss=P, loss=P, dX=P, dW=P, n=1, on=h):
+    def ce(X=P, W=P, targets=P, dloss=2 * P, loss=P, dX=P, dW=P, n=1, on=h):
         return lib.aq_loss_cross_entropy(on, X, W, targets, dloss, loss, dX, dW, n, None)
 
     def di(logits=P, ids=P, teacher=P, top=2, T=1.0, dloss=P, loss=P, dlogits=P, n=1, on=h):
@@ -128,7 +128,9 @@ def loss_calls():
 
     for f, kws in ((ce, [dict(X=None), dict(W=None), dict(targets=None), dict(loss=None), dict(n=0), dict(n=9),
                          dict(X=P + 2), dict(W=P + 8), dict(dX=P + 4), dict(dW=P + 8), dict(targets=P + 4),
-                         dict(dloss=P + 2), dict(loss=P + 1), dict(on=plain), {}, dict(dX=None, dW=None, dloss=None, n=8)]),
+                         dict(dloss=P + 2), dict(loss=P + 1), dict(on=plain), dict(dloss=P), dict(dloss=P + 28, n=8),
+                         dict(dloss=P - 28, n=8), dict(dloss=P + 32, n=8), {},
+                         dict(dX=None, dW=None, dloss=None, n=8)]),
                    (di, [dict(logits=None), dict(ids=None), dict(teacher=None), dict(loss=None), dict(n=0), dict(n=9),
                          dict(top=0), dict(top=1025), dict(T=0.0), dict(T=-1.0), dict(T=float("inf")),
                          dict(T=float("nan")), dict(logits=P + 8), dict(dlogits=P + 2), dict(ids=P + 2),
@@ -182,7 +184,8 @@ def test_loss_calls_refuse(so):
     out, left = host_device.in_child(so, "test_usq_losses_host", "loss_calls")
     I, S = A.AQ_ERR_INVALID_ARGUMENT, A.AQ_ERR_UNSUPPORTED
     want = [(I, "null")] * 4 + [(I, "n must be"), (I, "max_tokens")] + [(I, "16-byte")] * 4 + [
-        (I, "8-byte"), (I, "4-byte"), (I, "4-byte"), (I, "without features"), (0, ""), (0, "")]
+        (I, "8-byte"), (I, "4-byte"), (I, "4-byte"), (I, "without features")] + [
+        (I, "overlaps")] * 3 + [(0, "")] * 3
     want += [(I, "null")] * 4 + [(I, "n must be"), (I, "max_tokens"), (I, "top"), (S, "top")] + [(I, "temperature")] * 4 + [
         (I, "16-byte"), (I, "16-byte"), (I, "aligned"), (I, "aligned"), (I, "aligned"), (0, ""), (0, "")]
     assert [s for s, _ in out] == [s for s, _ in want]
