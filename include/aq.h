@@ -390,8 +390,9 @@ aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* 
  * Forward Y = X * W^T on `stream`; asynchronous, allocates nothing and never
  * synchronises.  Weights are not rounded: the codes are multiplied with the
  * inputs exactly, sums are fp32, and each group's sum is scaled, its zero
- * point times the sum of the group's inputs taken off (inputs so large that 15
- * times a group's sum passes fp32 give infinities or NaN).
+ * point times the sum of the group's inputs taken off (infinite inputs, and
+ * inputs so large that 15 times a group's sum passes fp32, give infinities or
+ * NaN in their own token's outputs).
  * Summation orders are fixed for each n: repeated calls give identical bits.
  *   X   device [n][in_features] in desc->dtype; 16-byte aligned
  *   Y   device [n][out_features] in desc->y_dtype; 16-byte aligned
@@ -415,7 +416,7 @@ aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void*
  * sums, and, unless out_features is a multiple of 8, a copy of dY for
  * max_tokens tokens.  Later calls are asynchronous and allocate nothing.
  * Gradients of one layer share that workspace: serialise them on one stream.
- * Errors and determinism as for aq_usq_forward.
+ * dY and dX must not overlap.  Errors and determinism as for aq_usq_forward.
  */
 aq_status aq_usq_input_grad(aq_usq* layer, const void* dY, void* dX, int64_t n, void* stream);
 

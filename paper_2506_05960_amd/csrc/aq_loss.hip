@@ -744,6 +744,8 @@ aq_status aq_loss_cross_entropy(aq_loss* L, const void* X, const void* W, const 
     const int64_t F = L->desc.features, tiles_n = (n + 127) / 128;
     if (tiles_n * ((L->desc.vocab + 127) / 128) > aq::kMaxTiles || tiles_n * ((F + 127) / 128) > aq::kMaxTiles)
         return api_fail(AQ_ERR_UNSUPPORTED, "too many tokens times vocabulary or features for one call");
+    if (dW && ((n + 63) / 64 * ((F + 63) / 64) + n / 4 + 2 >= (1 << 24)))    // the joining launch's workgroups
+        return api_fail(AQ_ERR_UNSUPPORTED, "too many tokens times features for one call");
     if (dX || dW) {
         s = grad_workspace(L, dX != nullptr, dW != nullptr, stream);
         if (s != AQ_OK) return s;

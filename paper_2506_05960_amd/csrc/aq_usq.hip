@@ -69,31 +69,35 @@ struct UsqArgs {
     int cps;               // chunks a split
 };
 
+// (a launch holds fewer than 2^32 threads, and no more than this many blocks of them are of use)
+constexpr int64_t kLayoutBlocks = 1 << 20;
+unsigned layout_blocks(int64_t count) { return (unsigned)std::min((count + 255) / 256, kLayoutBlocks); }
+
 // Packed codes as the caller has them ([C_out][K / 2], the lower half first) into the device layout.
 __global__ void __launch_bounds__(256) usq_pack_kernel(const uint8_t* src, uint32_t* dst, int C_out, int K, int nchunk,
                                                        int64_t words) {
-    const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (w >= words) return;
-    const int s = (int)(w & 3), lane = (int)(w >> 2) & 63;
-    const int64_t tile = w >> 8;
-    const int c = (int)(tile % nchunk);
-    const int64_t i = tile / nchunk * 16 + (lane & 15);
-    const int k = c * 128 + s * 32 + (lane >> 4) * 8;
-    uint32_t v = 0, o = 0;
-    if (i < C_out && k < K) v = *reinterpret_cast<const uint32_t*>(src + i * (K / 2) + k / 2);
+    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < words; w += (int64_t)gridDim.x * 256) {
+        const int s = (int)(w & 3), lane = (int)(w >> 2) & 63;
+        const int64_t tile = w >> 8;
+        const int c = (int)(tile % nchunk);
+        const int64_t i = tile / nchunk * 16 + (lane & 15);
+        const int k = c * 128 + s * 32 + (lane >> 4) * 8;
+        uint32_t v = 0, o = 0;
+        if (i < C_out && k < K) v = *reinterpret_cast<const uint32_t*>(src + i * (K / 2) + k / 2);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o |= ((v >> (4 * e)) & 15u) << (8 * (e & 3) + 4 * (e >> 2));
-    dst[w] = o;
+        for (int e = 0; e < 8; ++e) o |= ((v >> (4 * e)) & 15u) << (8 * (e & 3) + 4 * (e >> 2));
+        dst[w] = o;
+    }
 }
 
 // [C_out][G] -> [row tile][groups][16], zero past the ends.
 template <typename T>
 __global__ void __launch_bounds__(256) usq_groups_kernel(const T* src, T* dst, int C_out, int G, int groups, int64_t count) {
-    const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (w >= count) return;
-    const int64_t i = w / (16 * (int64_t)groups) * 16 + (w & 15);
-    const int j = (int)(w / 16 % groups);
-    dst[w] = i < C_out && j < G ? src[i * G + j] : T(0);
+    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < count; w += (int64_t)gridDim.x * 256) {
+        const int64_t i = w / (16 * (int64_t)groups) * 16 + (w & 15);
+        const int j = (int)(w / 16 % groups);
+        dst[w] = i < C_out && j < G ? src[i * G + j] : T(0);
+    }
 }
 
 // The eight codes of a word as 16-bit floats in value order.  A byte b below 16
@@ -841,7 +845,7 @@ constexpr size_t kSplitBytes = size_t(64) << 20;   // and the input gradient's
 aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t* zeros) {
     const aq_usq_desc& d = L->desc;
     const int64_t tiles = (d.out_features + 15) / 16;
-    const int G = (d.in_features + d.group - 1) / d.group;
+    const int G = (int)((d.in_features + (int64_t)d.group - 1) / d.group);
     const size_t code_bytes = (size_t)d.out_features * (d.in_features / 2), group_count = (size_t)d.out_features * G;
     const int64_t words = tiles * L->nchunk * 256, count = tiles * L->groups * 16;
     aq_status s = alloc(&L->d_codes, (size_t)words * 4, "codes");
@@ -867,13 +871,13 @@ aq_status upload(aq_usq* L, const void* codes, const void* scales, const uint8_t
     hipError_t e = hipMemset(L->d_zero, 0, 256);
     if (e == hipSuccess) e = hipMemcpy(tmp, codes, code_bytes, hipMemcpyHostToDevice);
     if (e == hipSuccess) {
-        aq::usq_pack_kernel<<<(unsigned)((words + 255) / 256), 256, 0, nullptr>>>(tmp, L->d_codes, d.out_features,
-                                                                                 d.in_features, L->nchunk, words);
+        aq::usq_pack_kernel<<<aq::layout_blocks(words), 256, 0, nullptr>>>(tmp, L->d_codes, d.out_features,
+                                                                          d.in_features, L->nchunk, words);
         e = hipGetLastError();
     }
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e == hipSuccess) e = hipMemcpy(tmp, scales, group_count * 2, hipMemcpyHostToDevice);
-    const unsigned blocks = (unsigned)((count + 255) / 256);
+    const unsigned blocks = aq::layout_blocks(count);
     if (e == hipSuccess) {
         aq::usq_groups_kernel<uint16_t><<<blocks, 256, 0, nullptr>>>(reinterpret_cast<const uint16_t*>(tmp), L->d_scales,
                                                                    d.out_features, G, L->groups, count);

@@ -166,6 +166,17 @@ def usq_limits(n, K, C_out):
     return got
 
 
+def usq_one_group():
+    """Creation and calls of a layer whose group is the largest there is: one scale a row."""
+    lib = _lib()
+    live = host_device.live_bytes()
+    st, h, msg = _create_usq(group=(1 << 31) - 128)
+    assert st == A.AQ_OK, msg
+    got = [host_device.live_bytes() - live, lib.aq_usq_forward(h, 4096, 4096, 1, None), lib.aq_usq_input_grad(h, 4096, 4096, 1, None)]
+    lib.aq_usq_destroy(h)
+    return got
+
+
 @pytest.fixture(scope="module")
 def so(tmp_path_factory):
     _lib()
@@ -191,6 +202,11 @@ def test_loss_calls_refuse(so):
     assert [s for s, _ in out] == [s for s, _ in want]
     assert all(t in msg for (_, t), (_, msg) in zip(want, out))
     assert left == 0
+
+
+def test_usq_largest_group(so):
+    held, *got = host_device.in_child(so, "test_usq_losses_host", "usq_one_group")
+    assert got == [0, 0] and held < 1 << 20
 
 
 @pytest.mark.parametrize("n,features,vocab,top", [(1, 8, 1, 1), (70000, 64, 1000, 5), (3, 8, 3000000, 1024), (1 << 21, 8, 9, 1),
@@ -281,6 +297,15 @@ def test_loss_tensor_checks(host_tensors):
         args.update(kw)
         with pytest.raises(ValueError, match=text):
             L.distill(**args)
+
+
+def test_descriptors_refuse_what_would_wrap():
+    with pytest.raises(ValueError, match="2\\^31"):
+        A.USQLayer(np.zeros((C_OUT, K // 2), np.uint8), np.ones((C_OUT, 1), np.float16), group=(1 << 32) + 32, max_tokens=4)
+    with pytest.raises(ValueError, match="2\\^31"):
+        A.VocabLoss((1 << 32) + 5, max_tokens=2)
+    with pytest.raises(ValueError, match="2\\^31"):
+        A.VocabLoss(5, features=(1 << 32) + 8, max_tokens=2)
 
 
 @pytest.mark.parametrize("kw", [dict(dtype="i8"), dict(features=0)])
