@@ -984,8 +984,12 @@ aq_status aq_usq_input_grad(aq_usq* L, const void* dY, void* dX, int64_t n, void
     const int C = L->desc.out_features;
     if (!L->cp) {
         L->cp = (C + 7) / 8 * 8;
-        const int64_t most = std::max<int64_t>(128, (int64_t(16) << 20) / L->cp / 128 * 128);   // 32 MiB
-        L->slab = (int)std::min<int64_t>(most, (int64_t)L->nchunk * 128);
+        // Slabs of equal width and of at most 128 MiB, whole tiles of the product: the fewer there are the fewer of
+        // their products need K splits to fill the chip (4096 x 8192 -> 4096, two of 32 MiB 284 us, one 243; 64 tokens,
+        // 4096 -> 16384, four 124 us, one 60).
+        const int64_t padded = (int64_t)L->nchunk * 128, most = std::max<int64_t>(256, (int64_t(64) << 20) / L->cp);
+        const int64_t slabs = (padded + most - 1) / most;
+        L->slab = (int)std::min(padded, ((padded + slabs - 1) / slabs + 255) / 256 * 256);
     }
     if ((!L->d_wt || !L->d_dsum || (C % 8 != 0 && !L->d_dy)) && aq::capturing(static_cast<hipStream_t>(stream)))
         return api_fail(AQ_ERR_UNSUPPORTED, "the first input gradient allocates: not under graph capture");

@@ -134,9 +134,9 @@ def test_input_grad(n, K, C_out, group, dtype, zeros):
     assert torch.equal(lay.input_grad(dy.cuda()), got)
 
 
-def test_input_grad_in_slabs():
-    """A layer whose decoded weights pass the workspace's 32 MiB several times."""
-    n, K, C_out = 40, 1304, 40000
+@pytest.mark.parametrize("n, K, C_out", [(40, 1304, 40000), (5, 600, 125000)])
+def test_input_grad_in_slabs(n, K, C_out):
+    """Layers whose decoded weights come near the workspace's 128 MiB, and pass them."""
     codes, scales, z, W, _ = make(K, C_out, 128, "bf16", True)
     lay = layer_of(codes, scales, z, 128, "bf16", "bf16", n)
     dy = torch.randn(n, C_out, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
