@@ -438,7 +438,8 @@ typedef struct {
 } aq_loss_desc;
 
 /* Create the losses of one vocabulary on the current HIP device, with the row
- * statistics of the cross entropy: 8 bytes per token and 128 vocabulary rows.
+ * statistics of the cross entropy: 8 bytes per token and 128 vocabulary rows
+ * (and up to 1 MiB for distillation).
  * AQ_ERR_UNSUPPORTED: a vocabulary above 2^30, more than 2^24 tokens, or, for
  * the cross entropy, more than 2^21 features or tokens.  Every call needs the
  * handle's device to be the current one (AQ_ERR_INVALID_ARGUMENT). */
@@ -499,7 +500,9 @@ aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void*
  *   dlogits  device [n][vocab] in desc->dtype, overwritten; 16-byte aligned;
  *            may be `logits` itself; NULL: not computed
  *   n        1 <= n <= max_tokens
- * Asynchronous, allocates nothing; sums are fp32 in a fixed order.
+ * Asynchronous, allocates nothing; sums are fp32 in a fixed order for each n.
+ * Calls of up to 256 tokens use the handle's workspace: serialise them on one
+ * stream.
  */
 aq_status aq_loss_distill(aq_loss* loss_handle, const void* logits, const int32_t* ids, const void* teacher,
                           int32_t top, float temperature, const float* dloss, float* loss, void* dlogits, int64_t n,

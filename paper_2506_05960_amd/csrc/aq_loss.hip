@@ -16,6 +16,8 @@ struct aq_loss {
     int device;
     int piece;             // cross entropy: vocabulary rows a piece of the gradient covers
     uint8_t* d_zero;       // 256 zero bytes
+    float2* d_seg;         // distillation of few rows: [row][segment] maximum and sum of exponentials
+    float* d_list;         // and [row][top] the listed tokens' logits
     float2* d_part;        // [vocabulary tile of 128][max_tokens] maximum and sum of exponentials
     float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then {scale, 1 / scale}
     // gradient workspace, allocated by the first call that needs it
@@ -98,14 +100,24 @@ struct DistillArgs {
     int V, top;
     float c;               // log2(e) / temperature
     float T;
+    // rows in segments, a workgroup each
+    int segs, seg_vecs;    // segments a row, 16-byte vectors a segment
+    float2* part;          // [row][segment]
+    float* list;           // [row][top] the listed tokens' logits (the gradient may overwrite the logits)
 };
 
-// One workgroup a row.  The row's first NV 16-byte vectors of each thread stay in registers between the
+enum DistillPart {
+    DISTILL_ROW,           // a whole row: statistics, loss and gradient
+    DISTILL_STATS,         // a segment's maximum and sum
+    DISTILL_GRAD           // the loss, and a segment's gradient
+};
+
+// One workgroup a row, or a segment of one.  The first NV 16-byte vectors of each thread stay in registers between the
 // statistics and the gradient; a longer row's others are read twice.  Bound by memory: what is read or
 // written for the last time passes the caches by (non-temporal), so that the second reads find theirs there
 // (4096 x 131072 bf16: 542 -> 513 us, 4.2 TB/s of the 2.1 GB that cannot be done without).
-template <int DT, int THREADS, int NV>
-__device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t row) {
+template <int DT, int THREADS, int NV, DistillPart PART>
+__device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t row, const int seg) {
     constexpr int VEC = Store<DT>::kVec;
     constexpr int WAVES = THREADS / 64;
     __shared__ float s_m[WAVES], s_s[WAVES];
@@ -117,12 +129,17 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t 
     const int head = min(V, (int)((VEC - base % VEC) % VEC));
     const int nvec = (V - head) / VEC;
     const int tail0 = head + nvec * VEC;
+    // this workgroup's vectors; the first one takes what lies before and behind the row's
+    const int v0 = PART == DISTILL_ROW ? 0 : min(nvec, seg * a.seg_vecs);
+    const int v1 = PART == DISTILL_ROW ? nvec : min(nvec, v0 + a.seg_vecs);
+    const bool first = PART == DISTILL_ROW || seg == 0;
+    const bool lists = PART != DISTILL_STATS || first, reads = PART != DISTILL_GRAD || a.grad;
     const u32x4* body = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.logits) +
                                                        (base + head) * (16 / VEC));
     // the list first: its logits wait for its ids
     int32_t id0 = -1;
     float t0 = -INFINITY;
-    if (tid < top) {
+    if (lists && tid < top) {
         id0 = a.ids[row * top + tid];
         t0 = load_as_f32<DT>(a.teacher, row * top + tid);
     }
@@ -130,12 +147,16 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t 
     u32x4 held[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (tid + i * THREADS < nvec) held[i] = __builtin_nontemporal_load(&body[tid + i * THREADS]);
+        if (reads && v0 + tid + i * THREADS < v1) {
+            const u32x4* p = &body[v0 + tid + i * THREADS];
+            held[i] = PART == DISTILL_STATS ? *p : __builtin_nontemporal_load(p);
+        }
     // values before and behind the whole vectors: one a thread
-    const int edge = tid < head ? tid : tid < head + V - tail0 ? tail0 + tid - head : -1;
+    const int edge = !first ? -1 : tid < head ? tid : tid < head + V - tail0 ? tail0 + tid - head : -1;
     const float zedge = edge >= 0 ? load_as_f32<DT>(a.logits, base + edge) : -INFINITY;
     bool bad = false;                       // an id past the vocabulary
-    for (int j = tid; j < top; j += THREADS) {
+#pragma unroll 1
+    for (int j = lists ? tid : top; j < top; j += THREADS) {
         int32_t id = id0;
         float t = t0;
         if (j != tid) {
@@ -147,62 +168,83 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t 
             id = -1;
             t = -INFINITY;
         }
-        s_id[j] = id;
-        s_t[j] = t;
-        s_z[j] = id >= 0 ? load_as_f32<DT>(a.logits, base + id) : 0.0f;
+        if constexpr (PART == DISTILL_STATS) {
+            a.list[row * top + j] = id >= 0 ? load_as_f32<DT>(a.logits, base + id) : 0.0f;
+        } else {
+            s_id[j] = id;
+            s_t[j] = t;
+            s_z[j] = PART == DISTILL_GRAD ? a.list[row * top + j]
+                     : id >= 0            ? load_as_f32<DT>(a.logits, base + id)
+                                          : 0.0f;
+        }
     }
 
     // ---- maximum and sum of exponentials ----
     float m = zedge, s = edge >= 0 && zedge != -INFINITY ? 1.0f : 0.0f;
-    if (zedge != zedge) s = zedge;          // (a maximum passes over NaN)
-    auto add = [&](const float (&z)[VEC], float b) {
+    if constexpr (PART != DISTILL_GRAD) {
+        if (zedge != zedge) s = zedge;          // (a maximum passes over NaN)
+        auto add = [&](const float (&z)[VEC], float b) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) s += exp2_fast((z[e] - b) * a.c);
-    };
-    {
-        const float m0 = m;
+            for (int e = 0; e < VEC; ++e) s += exp2_fast((z[e] - b) * a.c);
+        };
+        {
+            const float m0 = m;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (tid + i * THREADS < nvec) {
-                float z[VEC];
-                unpack<DT>(held[i], z);
+            for (int i = 0; i < NV; ++i)
+                if (v0 + tid + i * THREADS < v1) {
+                    float z[VEC];
+                    unpack<DT>(held[i], z);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) m = fmaxf(m, z[e]);
-            }
-        const float b = m == -INFINITY ? 0.0f : m;
-        s *= exp2_fast((m0 - b) * a.c);
+                    for (int e = 0; e < VEC; ++e) m = fmaxf(m, z[e]);
+                }
+            const float b = m == -INFINITY ? 0.0f : m;
+            s *= exp2_fast((m0 - b) * a.c);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (tid + i * THREADS < nvec) {
-                float z[VEC];
-                unpack<DT>(held[i], z);
-                add(z, b);
-            }
-    }
-#pragma unroll 4
-    for (int v = tid + NV * THREADS; v < nvec; v += THREADS) {
-        float z[VEC];
-        unpack<DT>(body[v], z);
-        float vm = z[0];
-#pragma unroll
-        for (int e = 1; e < VEC; ++e) vm = fmaxf(vm, z[e]);
-        if (vm > m) {
-            s *= exp2_fast((m - vm) * a.c);
-            m = vm;
+            for (int i = 0; i < NV; ++i)
+                if (v0 + tid + i * THREADS < v1) {
+                    float z[VEC];
+                    unpack<DT>(held[i], z);
+                    add(z, b);
+                }
         }
-        add(z, m == -INFINITY ? 0.0f : m);
-    }
+#pragma unroll 4
+        for (int v = v0 + tid + NV * THREADS; v < v1; v += THREADS) {
+            float z[VEC];
+            unpack<DT>(body[v], z);
+            float vm = z[0];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), a.c);
-    if (lane == 0) {
-        s_m[wave] = m;
-        s_s[wave] = s;
-    }
-    bad = __syncthreads_or(bad);
-    m = s_m[0];
-    s = s_s[0];
+            for (int e = 1; e < VEC; ++e) vm = fmaxf(vm, z[e]);
+            if (vm > m) {
+                s *= exp2_fast((m - vm) * a.c);
+                m = vm;
+            }
+            add(z, m == -INFINITY ? 0.0f : m);
+        }
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) merge(m, s, s_m[w], s_s[w], a.c);
+        for (int o = 1; o < 64; o <<= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), a.c);
+        if (lane == 0) {
+            s_m[wave] = m;
+            s_s[wave] = s;
+        }
+        bad = __syncthreads_or(bad);
+        m = s_m[0];
+        s = s_s[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) merge(m, s, s_m[w], s_s[w], a.c);
+    }
+    if constexpr (PART == DISTILL_STATS) {
+        if (tid == 0) a.part[row * a.segs + seg] = make_float2(m, s);
+        return;
+    }
+    if constexpr (PART == DISTILL_GRAD) {
+        // (every wave joins the row's segments, at most a wave's lanes)
+        const float2 p = lane < a.segs ? a.part[row * a.segs + lane] : make_float2(-INFINITY, 0.0f);
+        m = p.x;
+        s = p.y;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), a.c);
+        bad = __syncthreads_or(bad);
+    }
     // log2 of a token's probability; the maximum leaves first, while the difference is exact or small
     const float ls = bad ? NAN : __builtin_amdgcn_logf(s);
     auto log2q = [&](float z) { return __builtin_fmaf(z - m, a.c, -ls); };
@@ -237,15 +279,15 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t 
         };
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (tid + i * THREADS < nvec) write(tid + i * THREADS, held[i]);
+            if (v0 + tid + i * THREADS < v1) write(v0 + tid + i * THREADS, held[i]);
 #pragma unroll 4
-        for (int v = tid + NV * THREADS; v < nvec; v += THREADS) write(v, body[v]);
+        for (int v = v0 + tid + NV * THREADS; v < v1; v += THREADS) write(v, body[v]);
         if (edge >= 0) store_as<DT>(a.grad, base + edge, value(zedge));
     }
 
     // ---- loss, and the listed tokens' gradient ----
     auto log2p = [&](int j) { return (s_t[j] - tb) * a.c - tl; };
-    if (wave == 0) {
+    if (first && wave == 0) {
         float l = 0.0f;
         for (int j = lane; j < top; j += 64) {
             const float lp = log2p(j), p = exp2_fast(lp);
@@ -260,18 +302,24 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t 
     // other threads wrote the listed tokens' values: every store has to be done before they are written again
     wait_vmcnt<0>();
     __syncthreads();
+#pragma unroll 1
     for (int j = tid; j < top; j += THREADS) {
         const int32_t id = s_id[j];
         if (id < 0) continue;
+        if (PART == DISTILL_GRAD) {         // another segment's?
+            const int v = (id - head) / VEC;
+            if (id < head || id >= tail0 ? !first : v < v0 || v >= v1) continue;
+        }
         // a token's first entry carries the mass of all of its entries
         float p = 0.0f;
-        bool first = true;
+        bool own = true;
+#pragma unroll 4
         for (int i = 0; i < top; ++i)
             if (s_id[i] == id) {
-                first &= i >= j;
+                own &= i >= j;
                 p += exp2_fast(log2p(i));
             }
-        if (first) store_as<DT>(a.grad, base + id, g * (exp2_fast(log2q(s_z[j])) - p));
+        if (own) store_as<DT>(a.grad, base + id, g * (exp2_fast(log2q(s_z[j])) - p));
     }
 }
 
@@ -280,9 +328,27 @@ constexpr int64_t kMaxRowBlocks = 1 << 20;
 template <int DT, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS, 4) distill_kernel(DistillArgs a) {
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        distill_row<DT, THREADS, NV>(a, row);
+        distill_row<DT, THREADS, NV, DISTILL_ROW>(a, row, 0);
         __syncthreads();
     }
+}
+
+// Few long rows, in segments: a launch for the statistics, and one that joins them and writes the gradient.  One
+// workgroup a row is bound by what a compute unit loads and exponentiates.
+constexpr int kMaxSegments = 1024, kMaxSegmentRows = 256;
+template <int DT, DistillPart PART>
+__global__ void __launch_bounds__(256, 4) distill_segment_kernel(DistillArgs a) {
+    const int row = (int)blockIdx.y;
+    distill_row<DT, 256, 4, PART>(a, row, (int)blockIdx.x);
+}
+
+template <int DT>
+hipError_t launch_distill_segments(const DistillArgs& a, hipStream_t st) {
+    distill_segment_kernel<DT, DISTILL_STATS><<<dim3((unsigned)a.segs, (unsigned)a.n), 256, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    distill_segment_kernel<DT, DISTILL_GRAD><<<dim3(a.grad ? (unsigned)a.segs : 1u, (unsigned)a.n), 256, 0, st>>>(a);
+    return hipGetLastError();
 }
 
 template <int DT, int THREADS, int NV>
@@ -614,10 +680,18 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
 }
 
 template <int DT>
-static hipError_t distill(const DistillArgs& a, hipStream_t st) {
+static hipError_t distill(DistillArgs a, hipStream_t st) {
+    // Up to 256 rows of 64 KB and more in segments, whole rows against segments: bf16, 1 x 131072 30.9 / 10.7 us,
+    // 16 x 131072 31.5 / 12.0, 200 x 131072 40.5 / 36.0, 16 x 32768 10.9 / 9.9, 200 x 32768 18.2 / 15.6; of 16 KB
+    // the second launch costs as much as it gives: 1 x 8000 7.6 / 9.9, 64 x 8000 13.9 / 12.5.
+    const int64_t vecs = a.V / Store<DT>::kVec;
+    if (a.n <= kMaxSegmentRows && vecs >= 4096) {
+        a.segs = (int)std::min<int64_t>(64, kMaxSegments / a.n);
+        a.seg_vecs = (int)((vecs + a.segs - 1) / a.segs);
+        return launch_distill_segments<DT>(a, st);
+    }
     // Rows of up to some 100 KB at four workgroups a compute unit, longer ones and few rows with more threads a row:
-    // 4096 x 32768 bf16 122 against 159 us, 1024 x 49999 fp16 50 against 53; 4096 x 131072 bf16 551 against 513,
-    // 4 x 32768 fp32 15.1 against 10.0.
+    // 4096 x 32768 bf16 122 against 159 us, 1024 x 49999 fp16 50 against 53; 4096 x 131072 bf16 551 against 513.
     return a.n >= 512 && (int64_t)a.V * (16 / Store<DT>::kVec) <= 100000 ? launch_distill<DT, 256, 16>(a, st)
                                                                         : launch_distill<DT, 512, 14>(a, st);
 }
@@ -627,7 +701,7 @@ static hipError_t distill(const DistillArgs& a, hipStream_t st) {
 namespace {
 
 void free_loss(aq_loss* L) {
-    void* ptrs[] = {L->d_zero, L->d_part, L->d_row, L->d_dlt, L->d_xt, L->d_dx};
+    void* ptrs[] = {L->d_seg, L->d_list, L->d_zero, L->d_part, L->d_row, L->d_dlt, L->d_xt, L->d_dx};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     delete L;
@@ -708,22 +782,25 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
         delete L;
         return api_hip_fail(e, "hipGetDevice");
     }
-    if (desc->features) {
+    const size_t few = (size_t)std::min<int64_t>(desc->max_tokens, aq::kMaxSegmentRows);
+    aq_status s = alloc(&L->d_seg, aq::kMaxSegments * sizeof(float2), "segment statistics");
+    if (s == AQ_OK) s = alloc(&L->d_list, few * aq::kMaxTop * sizeof(float), "listed logits");
+    if (s == AQ_OK && desc->features) {
         // a piece's gradient takes at most 128 MiB, its head rows too
         const int64_t most = std::min(aq::kMaxPitch, std::max<int64_t>(256, (int64_t(64) << 20) / std::max<int64_t>(
                                                                               desc->max_tokens, desc->features)));
         const int64_t pieces = (desc->vocab + most - 1) / most;
         L->piece = (int)(((desc->vocab + pieces - 1) / pieces + 255) / 256 * 256);
         const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 127) / 128;
-        aq_status s = alloc(&L->d_zero, 256, "zero block");
+        s = alloc(&L->d_zero, 256, "zero block");
         if (s == AQ_OK) s = alloc(&L->d_part, tiles * n * sizeof(float2), "row statistics");
         if (s == AQ_OK) s = alloc(&L->d_row, (4 * n + 2) * sizeof(float), "row state");
         if (s == AQ_OK && (e = hipMemset(L->d_zero, 0, 256)) != hipSuccess) s = api_hip_fail(e, "zero block");
         if (s == AQ_OK && (e = hipDeviceSynchronize()) != hipSuccess) s = api_hip_fail(e, "zero block");
-        if (s != AQ_OK) {
-            free_loss(L);
-            return s;
-        }
+    }
+    if (s != AQ_OK) {
+        free_loss(L);
+        return s;
     }
     *out = L;
     return AQ_OK;
@@ -776,7 +853,7 @@ aq_status aq_loss_distill(aq_loss* L, const void* logits, const int32_t* ids, co
     const aq_status s = check_call(L, n);
     if (s != AQ_OK) return s;
     const aq::DistillArgs a{logits, ids, teacher, dloss, loss, dlogits, n, L->desc.vocab, top, aq::kLog2e / temperature,
-                            temperature};
+                            temperature, 0, 0, L->d_seg, L->d_list};
     const auto st = static_cast<hipStream_t>(stream);
     const hipError_t e = L->desc.dtype == AQ_F32   ? aq::distill<AQ_F32>(a, st)
                          : L->desc.dtype == AQ_F16 ? aq::distill<AQ_F16>(a, st)

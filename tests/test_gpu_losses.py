@@ -159,6 +159,75 @@ def test_distill_in_place_and_without_gradient(n, vocab):
     assert same is work and torch.equal(again, loss) and torch.equal(work, grad)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_distill_few_long_rows(dtype):
+    """Rows that several workgroups share, at every offset from 16 bytes: listed tokens at both ends and at the ends of
+    16-byte groups all along, some twice; rows masked but for a few tokens at the front, in the middle, at the back;
+    a row without list; the gradient in place, alone and in graph replays."""
+    V, top, n = 70003, 520, 11
+    g = torch.Generator().manual_seed(21)
+    z = (torch.randn(n, V, generator=g) * 2).to(DT[dtype])
+    ids = torch.randint(0, V, (n, top), generator=g).int()
+    ends = torch.arange(0, V, 137)[:500].int()
+    ids[:, :500] = ends
+    ids[:, 500:505] = torch.tensor([V - 1, V - 2, V - 9, 0, 1], dtype=torch.int32)
+    t = torch.randn(n, top, generator=g).to(DT[dtype])
+    live = {1: range(0, 3), 2: range(35000, 35004), 3: range(V - 3, V), 4: [5, 40000, V - 1]}
+    for row, keep in live.items():
+        keep = list(keep)
+        z[row] = z[row].masked_fill(torch.ones(V, dtype=torch.bool).index_fill(0, torch.tensor(keep), False), -math.inf)
+        ids[row] = -1
+        ids[row, :len(keep)] = torch.tensor(keep, dtype=torch.int32)
+    ids[5] = -1
+    dloss = torch.rand(n, generator=g) + 0.5
+    L = losses(V, dtype=dtype, n=300)
+    zg, ig, tg, dg = z.cuda(), ids.cuda(), t.cuda(), dloss.cuda()
+    loss, grad = L.distill(zg, ig, tg, 1.5, dloss=dg, grad=True)
+    check_distill(z, ids, t, 1.5, dloss, dtype, loss, grad)
+    assert float(loss[5]) == 0 and bool((grad[5] == 0).all())
+    for row, keep in live.items():
+        assert int((grad[row] != 0).sum()) <= len(keep)
+    work = zg.clone()
+    again, _ = L.distill(work, ig, tg, 1.5, dloss=dg, grad=work)
+    assert torch.equal(again, loss) and torch.equal(work, grad)
+    assert torch.equal(L.distill(zg, ig, tg, 1.5, dloss=dg)[0], loss)
+    out, dz = torch.empty_like(loss), torch.empty_like(grad)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.distill(zg, ig, tg, 1.5, dloss=dg, loss=out, grad=dz)
+    for _ in range(3):
+        L.distill(zg[:3], ig[:3], tg[:3], 1.0)                    # the workspace of another size in between
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, loss) and torch.equal(dz, grad)
+        out.zero_()
+        dz.zero_()
+
+
+@pytest.mark.parametrize("n", [1, 17, 64, 65, 255, 256, 257])
+def test_distill_row_counts(n):
+    """A row's loss does not depend on how many rows there are, beyond the order of its sums."""
+    V, top = 33003, 7
+    g = torch.Generator().manual_seed(n)
+    z = torch.randn(1, V, generator=g).to(torch.bfloat16)
+    ids = torch.randint(0, V, (1, top), generator=g).int()
+    t = torch.randn(1, top, generator=g).to(torch.bfloat16)
+    loss, grad = losses(V, n=n).distill(z.repeat(n, 1).cuda(), ids.repeat(n, 1).cuda(), t.repeat(n, 1).cuda(), grad=True)
+    check_distill(z, ids, t, 1.0, torch.ones(1), "bf16", loss[-1:], grad[-1:])
+    assert bool((loss - loss[0]).abs().max() <= 2e-5) and bool((grad.float() - grad[0].float()).abs().max() <= 2.0 ** -8)
+
+
+def test_distill_bad_rows_show_in_segments():
+    V = 40001
+    z, t = torch.randn(4, V, device="cuda"), torch.randn(4, 2, device="cuda")
+    z[1, 39000] = float("nan")
+    z[3, 100] = float("inf")
+    ids = torch.tensor([[5, 6], [5, 6], [5, V], [7, 8]], dtype=torch.int32, device="cuda")
+    loss, grad = losses(V, dtype="f32", n=4).distill(z, ids, t, grad=True)
+    assert bool(loss[0].isfinite()) and bool(grad[0].isfinite().all())
+    assert bool(loss[1:3].isnan().all()) and bool(grad[1:3].isnan().all()) and not bool(loss[3].isfinite())
+
+
 def test_distill_gradient_matches_differences():
     """Central differences of the loss in fp32: their own error is the third-order term, |step|^2 / 6 of a smooth
     function whose third derivatives are at most 1, plus the losses' rounding over the step."""
