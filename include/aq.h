@@ -412,7 +412,7 @@ aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void*
  *   dX  device [n][in_features] in desc->dtype, overwritten; 16-byte aligned
  * The first call on a layer allocates its workspace (synchronous; refused with
  * AQ_ERR_UNSUPPORTED on a stream under graph capture): the decoded weights of a
- * slab of inputs, some 128 MiB (or of 256 inputs), at most 64 MiB of partial
+ * slab of inputs (for more than 64 tokens), some 128 MiB (or of 256 inputs), at most 64 MiB of partial
  * sums, and, unless out_features is a multiple of 8, a copy of dY for
  * max_tokens tokens.  Later calls are asynchronous and allocate nothing.
  * Gradients of one layer share that workspace: serialise them on one stream.

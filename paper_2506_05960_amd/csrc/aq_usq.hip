@@ -779,6 +779,8 @@ __global__ void __launch_bounds__(256) usq_decode_t_kernel(UsqArgs a, int group,
 // inputs (rounded once to 16 bits, as above) into an LDS buffer of its own, and
 // transposing reads deliver them with the rows as the summed index.  The waves
 // add their sums in LDS in wave order, the splits through split_sum_kernel.
+// Bound by the decode (fp32 per weight) and, with the tokens, by the loads of dY,
+// whose lanes lie on different tokens, and the splits' sums.
 // SG: steps of 32 inputs a scale group, as in usq_few_kernel.
 constexpr int kGradRows = 32, kGradPitch = 272;     // a row's 256 bytes and 16: rows start in different banks
 template <int DT, int SG, int NT>
@@ -877,11 +879,15 @@ __global__ void __launch_bounds__(256) usq_few_grad_kernel(UsqArgs a, const uint
     }
 }
 
-// Rows a split: whole steps of the four waves, splits for some 1024 workgroups within `cap` bytes of sums.
+// Rows a split: whole steps of the four waves; splits for one workgroup a compute unit, or two of layers that leave
+// them four steps each, within `cap` bytes of sums.  us with 256 / 512 / 1024 workgroups: 4096 -> 4096, 1 token 10.6 /
+// 10.5 / 11.5, 16 tokens 11.6 / 12.3 / 15.0, 64 tokens 17.5 / 21.9 / 27.6; 4096 -> 16384, 1 token 24.9 / 21.5 / 20.8,
+// 64 tokens 32.3 / 31.6 / 38.7 (through W in memory 27 to 32 and 58 to 60).
 int few_grad_rows(int n, int K, int cp, size_t cap) {
     const int chunks = (K + 127) / 128, steps = (cp + 4 * kGradRows - 1) / (4 * kGradRows);
     const int64_t fit = (int64_t)(cap / ((size_t)n * K * 4));
-    const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, fit), 1024 / chunks));
+    const int wgs = (int64_t)steps * chunks >= 2048 ? 512 : 256;
+    const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, fit), wgs / chunks));
     return (steps + splits - 1) / splits * 4 * kGradRows;
 }
 
