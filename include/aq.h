@@ -467,7 +467,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
  *            aligned; NULL: not computed
  *   n        1 <= n <= max_tokens
  * Sums are fp32; dz is rounded once to desc->dtype before the products (scaled
- * so that the largest |dloss| lies just below 2^15).
+ * so that its largest entry at a target is exact, just below 2^15).
  * dX, dW and loss must overlap nothing else (a loss that overlaps dloss is
  * refused).
  * The first call with dX or with dW allocates its workspace (synchronous;

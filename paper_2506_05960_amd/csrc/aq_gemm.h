@@ -305,18 +305,27 @@ __device__ __forceinline__ void gemm_mainloop(const GemmOperands& g, int m0, int
 // of the same output add to.  With K split over workgroups every split keeps a
 // sum of its own, and split_sum_kernel adds them.
 enum StoreMode {
-    STORE_OUT = 0,         // out = D * scale
+    STORE_OUT = 0,         // out = D, unscaled
     STORE_SUM = 1,         // sum = D
     STORE_ADD = 2,         // sum += D
-    STORE_LAST = 3         // out = (sum + D) * scale
+    STORE_LAST = 3         // out = sum + D, unscaled
 };
+
+// The logits' gradient is stored in 16 bits, scaled so that its largest entry at a target, `peak`, lies at 32640 =
+// 255 * 2^7, which fp16 and bf16 hold exactly, near the end of a binade.  fp16 then keeps its relative precision
+// whatever the losses' weights, and the entries that make most of a row's gradient, which share one rounding, round
+// with half the error of the worst scale (the largest with none).
+constexpr float kGradPeak = 32640.0f;
+__device__ __forceinline__ bool peak_fits(float peak) { return peak > 0x1p-100f; }      // (a quotient below would overflow)
+__device__ __forceinline__ float grad_scale(float peak) { return peak_fits(peak) ? kGradPeak / peak : 1.0f; }
+__device__ __forceinline__ float grad_unscale(float peak) { return peak_fits(peak) ? peak / kGradPeak : 1.0f; }
 
 template <int DT>
 struct StoreArgs {
     uint16_t* out;         // [M] rows of pitch ldo
     float* sum;            // [split][M][N]
     int64_t ldo;           // at most kMaxPitch, as N is
-    const float* scale;    // null: 1
+    const float* peak;     // of a scaled gradient; null: D as it is
 };
 
 template <int DT, int MODE, int WM, int WN, int AM, int AN>
@@ -329,7 +338,7 @@ struct StoreEpilogue {
         constexpr bool kOut = MODE == STORE_OUT || MODE == STORE_LAST, kOld = MODE == STORE_ADD || MODE == STORE_LAST;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
-        const float f = kOut && s.scale ? *s.scale : 1.0f;
+        const float f = kOut && s.peak ? grad_unscale(*s.peak) : 1.0f;
         const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(s.out + (int64_t)m0 * s.ldo + n0, kOutOfRange);
         const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(s.sum + ((int64_t)z * M + m0) * N + n0, kOutOfRange);
 #pragma unroll
@@ -431,11 +440,11 @@ hipError_t launch_store_gemm(const GemmOperands& g, const GemmPlan& p, const Sto
                  : launch_gemm<DT, 2, 2, 2, 2, TR>(g, p, StoreEpilogue<DT, MODE, 2, 2, 2, 2>{s}, st);
 }
 
-// out[m][n] = scale * (sum over the splits, in split order), four values a thread (N a multiple of 8).
+// out[m][n] = unscaled (sum over the splits, in split order), four values a thread (N a multiple of 8).
 template <int DT>
 __global__ void __launch_bounds__(256) split_sum_kernel(const float* sum, int splits, int64_t M, int N, uint16_t* out,
-                                                        int64_t ldo, const float* scale) {
-    const float f = scale ? *scale : 1.0f;
+                                                        int64_t ldo, const float* peak) {
+    const float f = peak ? grad_unscale(*peak) : 1.0f;
     const int64_t count = M * N;
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)gridDim.x * 1024) {
         floatx4 v = *reinterpret_cast<const floatx4*>(sum + i);
@@ -450,9 +459,9 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const float* sum, int sp
 
 template <int DT>
 hipError_t launch_split_sum(const float* sum, int splits, int64_t M, int N, uint16_t* out, int64_t ldo,
-                            const float* scale, hipStream_t st) {
+                            const float* peak, hipStream_t st) {
     const int64_t blocks = (M * N + 1023) / 1024;
-    split_sum_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, scale);
+    split_sum_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, peak);
     return hipGetLastError();
 }
 

@@ -19,7 +19,7 @@ struct aq_loss {
     float2* d_seg;         // distillation of few rows: [row][segment] maximum and sum of exponentials
     float* d_list;         // and [row][top] the listed tokens' logits
     float2* d_part;        // [vocabulary tile of 128][max_tokens] maximum and sum of exponentials
-    float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then {scale, 1 / scale}
+    float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then the peak
     // gradient workspace, allocated by the first call that needs it
     uint16_t* d_dlt;       // [piece][tokens] logits' gradient of a piece
     uint16_t* d_xt;        // [features][tokens] inputs, transposed
@@ -367,7 +367,7 @@ struct RowState {          // arrays of n tokens each
     float* ls;             // log2 of the sum of exponentials above it
     float* w;              // row weight of the gradient, 0 for a token that does not count
     float* loss;
-    float* scale;          // {scale, 1 / scale} of the stored logits' gradient
+    float* peak;           // the largest entry of the logits' gradient at a target
 };
 
 // D rows are vocabulary rows, D columns tokens: a lane's values all belong to
@@ -385,6 +385,7 @@ struct StatsEpilogue {
         float2* red = reinterpret_cast<float2*>(lds);            // [WM][BN]
         constexpr int BN = WN * AN * 32;
         __syncthreads();                                         // the last chunk is read
+        if (m0 == 0 && n0 == 0 && tid == 0) *rs.peak = 0.0f;
         const int v0 = m0 + wm * AM * 32 + 4 * hi;               // vocabulary row of register 0
         const bool edge = m0 + WM * AM * 32 > M;
 #pragma unroll
@@ -441,6 +442,10 @@ struct StatsEpilogue {
     }
 };
 
+__device__ __forceinline__ float row_weight(const RowState& rs, int64_t t) {
+    return rs.targets[t] < 0 ? 0.0f : rs.dloss ? rs.dloss[t] : 1.0f;
+}
+
 // dloss (P - 1 at the target) of a piece of the vocabulary, in 16 bits, as
 // [row][token].  Tokens up to a multiple of 8 and rows up to the tile's end are
 // written (zeros past the ends): the products that read them walk whole 16-byte
@@ -456,7 +461,7 @@ struct GradEpilogue {
     __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int, int m0, int n0, int M, int N, uint8_t*) const {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
-        const float scale = rs.scale[0];
+        const float scale = grad_scale(*rs.peak);
         const bool odd = lane & 1;
         // the tile's rows from its corner: at most 255 pitches of kMaxPitch
         const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(dlt + (int64_t)m0 * np + n0, kOutOfRange);
@@ -491,30 +496,6 @@ struct GradEpilogue {
         }
     }
 };
-
-// Factor that takes the largest row weight just below 2^15.  Stored gradients of an fp16 model then keep fp16's
-// relative precision whatever the weights' size, and the target's entry, (p - 1) times the weight and often the
-// largest of its row, lies where the type's steps are finest relative to it (equal weights: half the error of the
-// worst factor).
-__device__ __forceinline__ float row_weight(const RowState& rs, int64_t t) {
-    return rs.targets[t] < 0 ? 0.0f : rs.dloss ? rs.dloss[t] : 1.0f;
-}
-
-__device__ __forceinline__ void find_scale(const RowState& rs, int n) {
-    __shared__ float red[4];
-    float m = 0.0f;
-    for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, fabsf(row_weight(rs, i)));
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int i = 1; i < 4; ++i) m = fmaxf(m, red[i]);
-    // (the quotient of a weight below 2^-100 would overflow)
-    const bool fits = m > 0x1p-100f && m < INFINITY;
-    rs.scale[0] = fits ? 32760.0f / m : 1.0f;
-    rs.scale[1] = fits ? m / 32760.0f : 1.0f;
-}
 
 // dst[c][r] = src[r][c] for r < R, zero for R <= r < pitch and for rows that do not count.
 struct Transpose {
@@ -569,42 +550,48 @@ __device__ __forceinline__ void join_tokens(const RowState& rs, const float2* pa
         }
     red[p][tok] = make_float2(m, s);
     __syncthreads();
-    if (p != 0 || t >= n) return;
+    if (p != 0) return;
+    float peak = 0.0f;
+    if (t < n) {
 #pragma unroll 8
-    for (int w = 1; w < kParts; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
-    const int64_t target = rs.targets[t];
-    float ls = __builtin_amdgcn_logf(s);
-    float w = rs.dloss ? rs.dloss[t] : 1.0f;
-    float l = 0.0f;
-    if (target < 0) {
-        w = 0.0f;
-    } else if (target >= V) {
-        ls = l = NAN;
-    } else {
-        l = (m - rs.zt[t]) + kLn2 * ls;
+        for (int w = 1; w < kParts; ++w) merge(m, s, red[w][tok].x, red[w][tok].y, kLog2e);
+        const int64_t target = rs.targets[t];
+        float ls = __builtin_amdgcn_logf(s);
+        const float w = row_weight(rs, t);
+        float l = 0.0f;
+        if (target >= V) {
+            ls = l = NAN;
+        } else if (target >= 0) {
+            l = (m - rs.zt[t]) + kLn2 * ls;
+            // (below 2^-20 of the weight the difference from 1 is rounding)
+            const float v = fabsf(w) * fmaxf(1.0f - exp2_fast(__builtin_fmaf(rs.zt[t] - m, kLog2e, -ls)), 0x1p-20f);
+            if (v < INFINITY) peak = v;
+        }
+        rs.loss[t] = l;
+        rs.top[t] = m;
+        rs.ls[t] = ls;
+        rs.w[t] = w;
     }
-    rs.loss[t] = l;
-    rs.top[t] = m;
-    rs.ls[t] = ls;
-    rs.w[t] = w;
+#pragma unroll
+    for (int o = 1; o < TOK; o <<= 1) peak = fmaxf(peak, __shfl_xor(peak, o));
+    // (bits of positive floats are in their order, and a maximum does not depend on the order of its arguments)
+    if (tok == 0 && peak > 0.0f) atomicMax(reinterpret_cast<unsigned*>(rs.peak), __float_as_uint(peak));
 }
 
-// Between the statistics and the gradient, in one launch: the tokens' joins, and what the gradient's products need
-// beside the logits: for dW the transposed inputs (rows that do not count left out: zeros times what they hold may not
-// reach dW), and the scale.
+// Between the statistics and the gradient, in one launch: the tokens' joins, and for dW the transposed inputs (rows
+// that do not count left out: zeros times what they hold may not reach dW).
 template <int TOK>
 __global__ void __launch_bounds__(256) join_kernel(RowState rs, const float2* part, int tiles, int n, int64_t V,
                                                    Transpose x) {
     const int joins = (n + TOK - 1) / TOK, b = (int)blockIdx.x;
     if (b < joins) join_tokens<TOK>(rs, part, tiles, n, V);
-    else if (b < joins + x.tiles) transpose_tile(x, b - joins, rs);
-    else find_scale(rs, n);
+    else transpose_tile(x, b - joins, rs);
 }
 
 template <int TOK>
-hipError_t launch_join(const RowState& rs, const float2* part, int tiles, int n, int64_t V, const Transpose& x, bool grad,
+hipError_t launch_join(const RowState& rs, const float2* part, int tiles, int n, int64_t V, const Transpose& x,
                        hipStream_t st) {
-    const unsigned blocks = (unsigned)((n + TOK - 1) / TOK + (grad ? x.tiles + 1 : 0));
+    const unsigned blocks = (unsigned)((n + TOK - 1) / TOK + x.tiles);
     join_kernel<TOK><<<blocks, 256, 0, st>>>(rs, part, tiles, n, V, x);
     return hipGetLastError();
 }
@@ -634,8 +621,8 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     const int side = p.big ? 256 : 128;
     const int tiles_r = (np + 63) / 64;
     const Transpose tx = dW ? Transpose{X, L->d_xt, n, F, np, tiles_r, tiles_r * ((F + 63) / 64)} : Transpose{};
-    e = n > 64 ? launch_join<16>(rs, L->d_part, (V + side - 1) / side, n, V, tx, dX || dW, st)
-               : launch_join<4>(rs, L->d_part, (V + side - 1) / side, n, V, tx, dX || dW, st);
+    e = n > 64 ? launch_join<16>(rs, L->d_part, (V + side - 1) / side, n, V, tx, st)
+               : launch_join<4>(rs, L->d_part, (V + side - 1) / side, n, V, tx, st);
     if (e != hipSuccess || (!dX && !dW)) return e;
     const GemmPlan px = gemm_plan(n, F, std::min(V, piece), L->dx_bytes);
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
@@ -657,13 +644,13 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.N = F;
             d.K = rows;
             const bool whole = px.splits == 1 && last;
-            const StoreArgs<DT> s{dX, L->d_dx, F, rs.scale + 1};
+            const StoreArgs<DT> s{dX, L->d_dx, F, rs.peak};
             e = whole ? (first ? launch_store_gemm<DT, true, STORE_OUT>(d, px, s, st)
                                : launch_store_gemm<DT, true, STORE_LAST>(d, px, s, st))
                       : (first ? launch_store_gemm<DT, true, STORE_SUM>(d, px, s, st)
                                : launch_store_gemm<DT, true, STORE_ADD>(d, px, s, st));
             if (e == hipSuccess && last && !whole)
-                e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.scale + 1, st);
+                e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.peak, st);
             if (e != hipSuccess) return e;
         }
         if (dW) {
@@ -675,7 +662,7 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.N = F;
             d.K = np;
             e = launch_store_gemm<DT, false, STORE_OUT>(d, gemm_plan(rows, F, np, 0),
-                                                        StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.scale + 1}, st);
+                                                        StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.peak}, st);
             if (e != hipSuccess) return e;
         }
     }
@@ -797,7 +784,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
         const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 127) / 128;
         s = alloc(&L->d_zero, 256, "zero block");
         if (s == AQ_OK) s = alloc(&L->d_part, tiles * n * sizeof(float2), "row statistics");
-        if (s == AQ_OK) s = alloc(&L->d_row, (4 * n + 2) * sizeof(float), "row state");
+        if (s == AQ_OK) s = alloc(&L->d_row, (4 * n + 1) * sizeof(float), "row state");
         if (s == AQ_OK && (e = hipMemset(L->d_zero, 0, 256)) != hipSuccess) s = api_hip_fail(e, "zero block");
         if (s == AQ_OK && (e = hipDeviceSynchronize()) != hipSuccess) s = api_hip_fail(e, "zero block");
     }

@@ -333,6 +333,26 @@ def test_cross_entropy_weights_of_any_size(scale):
         check_ce(xh, wh, targets, dloss, "f16", *got)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("units", [1, 2, 3, 5, 8])
+def test_cross_entropy_stores_the_largest_target_entry_exactly(units, dtype):
+    """Two tokens, dz = +-q with q = dloss / (1 + e^gap): the stored entries are exact, and the gradients are off by
+    their own rounding, q's (`rel`: exponentials, sums and the difference from 1, 2^-23 over q) and the fp32 products'."""
+    F = 64
+    x, w = torch.zeros(1, F), torch.zeros(2, F)
+    x[0, :units], x[0, units:] = 0.5, 0
+    w[0, :units], w[1, :units] = 0.5, 0.25
+    w[:, units:] = torch.randint(-4, 5, (2, F - units), generator=torch.Generator().manual_seed(units)) / 4
+    dl = torch.tensor([0.7])
+    L = losses(2, features=F, dtype=dtype, n=1)
+    _, dx, dw = L.cross_entropy(x.to(DT[dtype]).cuda(), w.to(DT[dtype]).cuda(), torch.tensor([0], device="cuda"),
+                                dloss=dl.cuda(), dx=True, dw=True)
+    q = float(dl.double()) / (1 + math.exp(units / 8))
+    dz = torch.tensor([[-q, q]], dtype=torch.float64)
+    for got, want in ((dx, dz @ w.double()), (dw, dz.t() @ x.double())):
+        assert within(got, want, half_step(want, dtype) + want.abs() * (64 * U * (1 + 0.7 / q)))
+
+
 def test_cross_entropy_rows_that_do_not_count():
     n, F, V = 70, 64, 300
     x, w, targets, dloss = ce_inputs(n, F, V, "bf16", 2)
