@@ -373,7 +373,7 @@ struct RowState {          // arrays of n tokens each
 // D rows are vocabulary rows, D columns tokens: a lane's values all belong to
 // one token, so a tile's maximum and sum are reductions over registers.  4096 x
 // 4096 x 131072 bf16: 3.27 ms, 1.34 PFLOP/s, bound by the products; 2048 x 1024
-// x 50021: 0.21 ms, 0.98 (16 chunks a tile, an exponential for every 1024 of K).
+// x 50021: 0.21 ms, 1.0 (16 chunks a tile, an exponential for every 1024 of K).
 template <int WM, int WN, int AM, int AN>
 struct StatsEpilogue {
     float2* part;          // [tiles_m][n]

@@ -409,9 +409,9 @@ __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
 //  * The zero points come first: -s z times the group sums is a product over
 //    groups, of s z in two bf16 pieces (15 bits at most, exact) and the sums in
 //    three, six of the eight values a lane holds for one group.
-// Bound by issue slots and the clock under load: besides 64 matrix instructions
+// Bound by issue slots and the clock under load: besides 32 matrix instructions
 // a chunk takes a wave 56 instructions that widen and 64 that scale.  4096 x
-// 4096 -> 4096 bf16, group 128: 135 us of a 142 us call, 1.0 PFLOP/s.
+// 4096 -> 4096 bf16, group 128: some 138 us of a 146 us call, 1.0 PFLOP/s.
 // SG: steps of 16 inputs a group within a chunk.
 template <int DT, int SG, int WM, int WN, int AM, int AN>
 __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
