@@ -496,7 +496,8 @@ aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void*
  *   teacher  device [n][top] in desc->dtype, the teacher's logits
  *   top      1 <= top <= 1024
  *   dloss    device [n] fp32; NULL: ones
- *   loss     device [n] fp32, overwritten; must overlap nothing else
+ *   loss     device [n] fp32, overwritten; must overlap nothing else (one that
+ *            overlaps dloss where other workgroups still read it is refused)
  *   dlogits  device [n][vocab] in desc->dtype, overwritten; 16-byte aligned;
  *            may be `logits` itself; NULL: not computed
  *   n        1 <= n <= max_tokens

@@ -669,13 +669,15 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     return hipSuccess;
 }
 
+// Up to 256 rows of 64 KB and more in segments, whole rows against segments: bf16, 1 x 131072 30.9 / 10.7 us,
+// 16 x 131072 31.5 / 12.0, 200 x 131072 40.5 / 36.0, 16 x 32768 10.9 / 9.9, 200 x 32768 18.2 / 15.6; of 16 KB
+// the second launch costs as much as it gives: 1 x 8000 7.6 / 9.9, 64 x 8000 13.9 / 12.5.
+static bool distill_segmented(int64_t n, int64_t V, int vec) { return n <= kMaxSegmentRows && V / vec >= 4096; }
+
 template <int DT>
 static hipError_t distill(DistillArgs a, hipStream_t st) {
-    // Up to 256 rows of 64 KB and more in segments, whole rows against segments: bf16, 1 x 131072 30.9 / 10.7 us,
-    // 16 x 131072 31.5 / 12.0, 200 x 131072 40.5 / 36.0, 16 x 32768 10.9 / 9.9, 200 x 32768 18.2 / 15.6; of 16 KB
-    // the second launch costs as much as it gives: 1 x 8000 7.6 / 9.9, 64 x 8000 13.9 / 12.5.
     const int64_t vecs = a.V / Store<DT>::kVec;
-    if (a.n <= kMaxSegmentRows && vecs >= 4096) {
+    if (distill_segmented(a.n, a.V, Store<DT>::kVec)) {
         a.segs = (int)std::min<int64_t>(64, kMaxSegments / a.n);
         a.seg_vecs = (int)((vecs + a.segs - 1) / a.segs);
         return launch_distill_segments<DT>(a, st);
@@ -727,7 +729,8 @@ aq_status grad_workspace(aq_loss* L, bool dx, bool dw, void* stream) {
     return s;
 }
 
-// Joined rows' losses are written while other workgroups still read dloss.
+// A loss is written while other workgroups still read dloss (joined rows of the cross entropy, segments of the
+// distillation; a whole row's own workgroup alone reads its dloss, and before it writes its loss).
 bool overlaps(const float* a, const float* b, int64_t n) { return a && b && a < b + n && b < a + n; }
 
 bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
@@ -842,6 +845,9 @@ aq_status aq_loss_distill(aq_loss* L, const void* logits, const int32_t* ids, co
         return api_fail(AQ_ERR_INVALID_ARGUMENT, "ids, teacher, dloss and loss must be aligned to their values");
     const aq_status s = check_call(L, n);
     if (s != AQ_OK) return s;
+    if (overlaps(loss, dloss, n) &&
+        (loss != dloss || aq::distill_segmented(n, L->desc.vocab, L->desc.dtype == AQ_F32 ? 4 : 8)))
+        return api_fail(AQ_ERR_INVALID_ARGUMENT, "loss overlaps dloss");
     const aq::DistillArgs a{logits, ids, teacher, dloss, loss, dlogits, n, L->desc.vocab, top, aq::kLog2e / temperature,
                             temperature, 0, 0, L->d_seg, L->d_list};
     const auto st = static_cast<hipStream_t>(stream);
