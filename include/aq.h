@@ -411,11 +411,15 @@ aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void*
  *   dY  device [n][out_features] in desc->dtype; 16-byte aligned
  *   dX  device [n][in_features] in desc->dtype, overwritten; 16-byte aligned
  * The first call on a layer allocates its workspace (synchronous; refused with
- * AQ_ERR_UNSUPPORTED on a stream under graph capture): the decoded weights of a
- * slab of inputs (for more than 64 tokens), some 128 MiB (or of 256 inputs), at most 64 MiB of partial
- * sums, and, unless out_features is a multiple of 8, a copy of dY for
- * max_tokens tokens.  Later calls are asynchronous and allocate nothing.
- * Gradients of one layer share that workspace: serialise them on one stream.
+ * AQ_ERR_UNSUPPORTED on a stream under graph capture), which the layer keeps:
+ *   - the weights decoded to 16 bits, of one slab of inputs, if max_tokens is
+ *     above 64 (or the sums below do not fit 64 MiB): all of them up to some
+ *     128 MiB, four times the bytes of their codes, and at least those of 256
+ *     inputs.  Each layer has its own;
+ *   - at most 64 MiB of partial sums;
+ *   - unless out_features is a multiple of 8, a copy of dY for max_tokens tokens.
+ * Later calls are asynchronous and allocate nothing.  Gradients of one layer
+ * share its workspace: serialise them on one stream.
  * dY and dX must not overlap.  Errors and determinism as for aq_usq_forward.
  */
 aq_status aq_usq_input_grad(aq_usq* layer, const void* dY, void* dX, int64_t n, void* stream);

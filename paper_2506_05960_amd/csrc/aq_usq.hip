@@ -1129,15 +1129,20 @@ aq_status aq_usq_input_grad(aq_usq* L, const void* dY, void* dX, int64_t n, void
         const int64_t slabs = (padded + most - 1) / most;
         L->slab = (int)std::min(padded, ((padded + slabs - 1) / slabs + 255) / 256 * 256);
     }
-    if ((!L->d_wt || !L->d_dsum || (C % 8 != 0 && !L->d_dy)) && aq::capturing(static_cast<hipStream_t>(stream)))
+    // W goes through memory for more than 64 tokens, and where the sums of the most few tokens do not fit
+    const int K = L->desc.in_features, few = (int)std::min<int64_t>(L->desc.max_tokens, aq::kFewTokens);
+    const size_t one = (size_t)few * K * 4;
+    const bool slabs = L->desc.max_tokens > aq::kFewTokens || one > kSplitBytes;
+    if (((slabs && !L->d_wt) || !L->d_dsum || (C % 8 != 0 && !L->d_dy)) && aq::capturing(static_cast<hipStream_t>(stream)))
         return api_fail(AQ_ERR_UNSUPPORTED, "the first input gradient allocates: not under graph capture");
-    s = alloc(&L->d_wt, (size_t)L->slab * L->cp * 2, "gradient workspace");
+    if (slabs) s = alloc(&L->d_wt, (size_t)L->slab * L->cp * 2, "gradient workspace");
     if (s == AQ_OK && !L->d_dsum) {
-        const int cols = std::min(L->slab, L->desc.in_features), tail = L->desc.in_features % L->slab;
-        size_t bytes = std::max<size_t>(16, aq::gemm_split_bytes(L->desc.max_tokens, cols, L->cp, kSplitBytes));
-        if (tail) bytes = std::max(bytes, aq::gemm_split_bytes(L->desc.max_tokens, tail, L->cp, kSplitBytes));
-        const int few = (int)std::min<int64_t>(L->desc.max_tokens, aq::kFewTokens), K = L->desc.in_features;
-        const size_t one = (size_t)few * K * 4;
+        size_t bytes = 16;
+        if (slabs) {
+            const int cols = std::min(L->slab, K), tail = K % L->slab;
+            bytes = std::max(bytes, aq::gemm_split_bytes(L->desc.max_tokens, cols, L->cp, kSplitBytes));
+            if (tail) bytes = std::max(bytes, aq::gemm_split_bytes(L->desc.max_tokens, tail, L->cp, kSplitBytes));
+        }
         if (one <= kSplitBytes) {
             const int rows = aq::few_grad_rows(few, K, L->cp, kSplitBytes);
             bytes = std::max(bytes, one * ((L->cp + rows - 1) / rows));

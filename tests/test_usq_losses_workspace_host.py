@@ -32,3 +32,36 @@ def distill_overlaps(vocab, dtype, n):
 def test_distillation_refuses_a_loss_over_dloss(so, vocab, dtype, n, at):
     got = host_device.in_child(so, "test_usq_losses_workspace_host", "distill_overlaps", vocab, dtype, n)
     assert got == [at, I, I, 0, 0]
+
+
+def usq_gradient_bytes(K, C_out, most):
+    """Bytes held after a layer's input gradients of 1, `most` and 17 tokens, and the splits (the second
+    dimension of the last launch of one workgroup column a chunk) of `most` tokens."""
+    lib, h = A.load_library(), ctypes.c_void_p()
+    d = A.aq_usq_desc(C_out, K, 128, A.AQ_F16, A.AQ_F16, most)
+    codes, scales = np.zeros((C_out, K // 2), np.uint8), np.zeros((C_out, -(-K // 128)), np.uint16)
+    assert lib.aq_usq_create(ctypes.byref(d), codes.ctypes.data, scales.ctypes.data, None, ctypes.byref(h)) == A.AQ_OK
+    live, got, splits = host_device.live_bytes(), [], 0
+    for n in (1, most, min(most, 17)):
+        st, launched = host_device.launches(lambda: lib.aq_usq_input_grad(h, 4096, 4096, n, None))
+        assert st == A.AQ_OK
+        got.append(host_device.live_bytes() - live)
+        if n == most:
+            splits = [y for x, y, *_ in launched if x == -(-K // 128)][-1]
+    lib.aq_usq_destroy(h)
+    return got, splits
+
+
+@pytest.mark.parametrize("K, C_out, most, slab", [
+    (4096, 16384, 64, False), (576, 1155, 64, False), (4096, 16384, 1, False), (1 << 20, 16, 1, False),
+    (576, 1155, 65, True), (4096, 4096, 4096, True), (1 << 20, 16, 64, True)])
+def test_layers_of_few_tokens_hold_no_decoded_weights(so, K, C_out, most, slab):
+    """Fp32 sums of each split and, for uneven rows, dY's copy; a slab is all of these layers' weights in 16 bits."""
+    got, splits = host_device.in_child(so, "test_usq_losses_workspace_host", "usq_gradient_bytes", K, C_out, most)
+    assert got[0] == got[1] == got[2]
+    padded = -(-C_out // 8) * 8
+    copy = 2 * most * padded if C_out % 8 else 0
+    if slab:
+        assert got[0] >= 2 * K * padded + copy
+    else:
+        assert got[0] == 4 * most * K * splits + copy
