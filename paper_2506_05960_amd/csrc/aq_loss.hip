@@ -288,15 +288,18 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, const int64_t 
     // ---- loss, and the listed tokens' gradient ----
     auto log2p = [&](int j) { return (s_t[j] - tb) * a.c - tl; };
     if (first && wave == 0) {
+        // T (log p - log q) = (t - tb) + (m - z) + T ln 2 (ls - tl): the logits enter as they are (times log2(e) / T, a
+        // logit at its type's lowest value would pass fp32), and their differences are exact or small
+        const float base = a.T * kLn2 * (ls - tl);
         float l = 0.0f;
         for (int j = lane; j < top; j += 64) {
-            const float lp = log2p(j), p = exp2_fast(lp);
-            if (p > 0.0f || p != p) l += p * (lp - log2q(s_z[j]));
+            const float p = exp2_fast(log2p(j));
+            if (p > 0.0f || p != p) l += p * ((s_t[j] - tb) + (m - s_z[j]) + base);
         }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
         if (bad) l = NAN;
-        if (lane == 0) a.loss[row] = counts ? a.T * a.T * kLn2 * l : 0.0f;
+        if (lane == 0) a.loss[row] = counts ? a.T * l : 0.0f;
     }
     if (!a.grad || !counts) return;
     // other threads wrote the listed tokens' values: every store has to be done before they are written again
