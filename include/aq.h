@@ -499,6 +499,8 @@ aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void*
  *            listed twice.  An id past the vocabulary makes its row NaN
  *   teacher  device [n][top] in desc->dtype, the teacher's logits
  *   top      1 <= top <= 1024
+ *   temperature  finite and positive (AQ_ERR_UNSUPPORTED below 2^-127, whose
+ *            reciprocal passes fp32)
  *   dloss    device [n] fp32; NULL: ones
  *   loss     device [n] fp32, overwritten; must overlap nothing else (one that
  *            overlaps dloss where other workgroups still read it is refused)

@@ -841,6 +841,7 @@ aq_status aq_loss_distill(aq_loss* L, const void* logits, const int32_t* ids, co
     if (top > aq::kMaxTop) return api_fail(AQ_ERR_UNSUPPORTED, "top above 1024");
     if (!(temperature > 0.0f) || !std::isfinite(temperature))
         return api_fail(AQ_ERR_INVALID_ARGUMENT, "temperature must be positive and finite");
+    if (!std::isfinite(aq::kLog2e / temperature)) return api_fail(AQ_ERR_UNSUPPORTED, "temperature below 2^-127");
     const unsigned b = L->desc.dtype == AQ_F32 ? 4 : 2;
     if (misaligned(logits, 16) || misaligned(dlogits, 16))
         return api_fail(AQ_ERR_INVALID_ARGUMENT, "logits and dlogits must be 16-byte aligned");

@@ -65,3 +65,17 @@ def test_layers_of_few_tokens_hold_no_decoded_weights(so, K, C_out, most, slab):
         assert got[0] >= 2 * K * padded + copy
     else:
         assert got[0] == 4 * most * K * splits + copy
+
+
+def temperatures(values):
+    lib, h = A.load_library(), ctypes.c_void_p()
+    assert lib.aq_loss_create(ctypes.byref(A.aq_loss_desc(300, 0, A.AQ_F32, 4)), ctypes.byref(h)) == A.AQ_OK
+    got = [lib.aq_loss_distill(h, 4096, 4096, 4096, 2, t, None, 4096, 4096, 4, None) for t in values]
+    lib.aq_loss_destroy(h)
+    return got
+
+
+def test_temperatures_without_a_finite_reciprocal_are_refused(so):
+    """log2(e) / T scales the logits: an infinity makes NaN of every row's largest logit."""
+    got = host_device.in_child(so, "test_usq_losses_workspace_host", "temperatures", [2.0 ** -149, 2.0 ** -128, 2.0 ** -127, 1e30])
+    assert got == [A.AQ_ERR_UNSUPPORTED, A.AQ_ERR_UNSUPPORTED, A.AQ_OK, A.AQ_OK]
