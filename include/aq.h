@@ -470,14 +470,17 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
  *   dW       device [vocab][features] in desc->dtype, overwritten; 16-byte
  *            aligned; NULL: not computed
  *   n        1 <= n <= max_tokens
- * Sums are fp32; dz is rounded once to desc->dtype before the products (scaled
- * so that its largest entry at a target is exact, just below 2^15).
+ * Sums are fp32; dz is rounded once to desc->dtype before the products, scaled
+ * so that an entry at a target is exact, just below 2^15: the call's largest,
+ * and in fp16, for dX, each token's own.  (So a row of dX keeps its precision
+ * whatever the other tokens' weights are; dW's in fp16 is relative to the
+ * call's largest weight, with 39 binades below it.)
  * dX, dW and loss must overlap nothing else (a loss that overlaps dloss is
  * refused).
  * The first call with dX or with dW allocates its workspace (synchronous;
  * refused with AQ_ERR_UNSUPPORTED on a stream under graph capture): 2 bytes
- * per token and vocabulary row of a piece (at most 128 MiB, or 256 rows), for
- * dX fp32 sums (4 bytes per token and feature unless one piece holds the
+ * per token and vocabulary row of a piece (at most 128 MiB, or 256 rows; twice
+ * that for both gradients in fp16), for dX fp32 sums (4 bytes per token and feature unless one piece holds the
  * vocabulary, or up to 64 MiB), for dW a copy of X.  Later calls are
  * asynchronous and allocate nothing.  Calls on one handle share its workspace:
  * serialise them on one stream.  Summation orders are fixed: repeated calls

@@ -311,11 +311,13 @@ enum StoreMode {
     STORE_LAST = 3         // out = sum + D, unscaled
 };
 
-// The logits' gradient is stored in 16 bits, scaled so that its largest entry at a target, `peak`, lies at 32640 =
-// 255 * 2^7, which fp16 and bf16 hold exactly, near the end of a binade.  fp16 then keeps its relative precision
-// whatever the losses' weights, and the entries that make most of a row's gradient, which share one rounding, round
-// with half the error of the worst scale (the largest with none).
+// The logits' gradient is stored in 16 bits, scaled so that an entry at a target, `peak`, lies at 32640 = 255 * 2^7,
+// which fp16 and bf16 hold exactly, near the end of a binade: the entries that make most of a row's gradient, which
+// share one rounding, then round with half the error of the worst scale (the peak with none).  For dW, and for both in
+// bf16, whose exponents are fp32's, it is the largest such entry of the call.  fp16 holds 39 binades below it, and
+// rows of far smaller weights would lose their small entries: for dX, whose rows stand apart, it is each token's own.
 constexpr float kGradPeak = 32640.0f;
+constexpr bool own_peaks(int dtype) { return dtype == AQ_F16; }       // dX's operand is scaled token by token
 __device__ __forceinline__ bool peak_fits(float peak) { return peak > 0x1p-100f; }      // (a quotient below would overflow)
 __device__ __forceinline__ float grad_scale(float peak) { return peak_fits(peak) ? kGradPeak / peak : 1.0f; }
 __device__ __forceinline__ float grad_unscale(float peak) { return peak_fits(peak) ? peak / kGradPeak : 1.0f; }
@@ -326,9 +328,11 @@ struct StoreArgs {
     float* sum;            // [split][M][N]
     int64_t ldo;           // at most kMaxPitch, as N is
     const float* peak;     // of a scaled gradient; null: D as it is
+    const float* own;      // peaks of D's rows instead (where they have their own)
 };
 
-template <int DT, int MODE, int WM, int WN, int AM, int AN>
+// OWN: D's rows have peaks of their own.
+template <int DT, int MODE, bool OWN, int WM, int WN, int AM, int AN>
 struct StoreEpilogue {
     StoreArgs<DT> s;
 
@@ -338,7 +342,7 @@ struct StoreEpilogue {
         constexpr bool kOut = MODE == STORE_OUT || MODE == STORE_LAST, kOld = MODE == STORE_ADD || MODE == STORE_LAST;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
-        const float f = kOut && s.peak ? grad_unscale(*s.peak) : 1.0f;
+        const float f = kOut && !OWN && s.peak ? grad_unscale(*s.peak) : 1.0f;
         const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(s.out + (int64_t)m0 * s.ldo + n0, kOutOfRange);
         const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(s.sum + ((int64_t)z * M + m0) * N + n0, kOutOfRange);
 #pragma unroll
@@ -346,6 +350,7 @@ struct StoreEpilogue {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int m = (wm * AM + a) * 32 + gemm_row(r, hi);
+                const float fm = kOut && OWN ? grad_unscale(s.own[min(m0 + m, M - 1)]) : f;
 #pragma unroll
                 for (int b = 0; b < AN; ++b) {
                     const int n = (wn * AN + b) * 32 + l32;
@@ -355,7 +360,7 @@ struct StoreEpilogue {
                     if (kOld) v += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, os, 0, 0));
                     if (kOut) {
                         const uint32_t oo = in ? (uint32_t)(m * (int)s.ldo + n) * 2u : kOutOfRange;
-                        __builtin_amdgcn_raw_buffer_store_b16(f32_to_tile<DT>(v * f), ro, oo, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b16(f32_to_tile<DT>(v * fm), ro, oo, 0, 0);
                     } else {
                         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rs, os, 0, 0);
                     }
@@ -436,21 +441,23 @@ hipError_t launch_gemm(GemmOperands g, const GemmPlan& p, const Epi& epi, hipStr
 
 template <int DT, bool TR, int MODE>
 hipError_t launch_store_gemm(const GemmOperands& g, const GemmPlan& p, const StoreArgs<DT>& s, hipStream_t st) {
-    return p.big ? launch_gemm<DT, 2, 4, 4, 2, TR>(g, p, StoreEpilogue<DT, MODE, 2, 4, 4, 2>{s}, st)
-                 : launch_gemm<DT, 2, 2, 2, 2, TR>(g, p, StoreEpilogue<DT, MODE, 2, 2, 2, 2>{s}, st);
+    constexpr bool kOwn = TR && own_peaks(DT);        // (transposed operands: dX)
+    return p.big ? launch_gemm<DT, 2, 4, 4, 2, TR>(g, p, StoreEpilogue<DT, MODE, kOwn, 2, 4, 4, 2>{s}, st)
+                 : launch_gemm<DT, 2, 2, 2, 2, TR>(g, p, StoreEpilogue<DT, MODE, kOwn, 2, 2, 2, 2>{s}, st);
 }
 
 // out[m][n] = unscaled (sum over the splits, in split order), four values a thread (N a multiple of 8).
 template <int DT>
 __global__ void __launch_bounds__(256) split_sum_kernel(const float* sum, int splits, int64_t M, int N, uint16_t* out,
-                                                        int64_t ldo, const float* peak) {
-    const float f = peak ? grad_unscale(*peak) : 1.0f;
+                                                        int64_t ldo, const float* peak, const float* own) {
+    const float call = peak ? grad_unscale(*peak) : 1.0f;
     const int64_t count = M * N;
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)gridDim.x * 1024) {
         floatx4 v = *reinterpret_cast<const floatx4*>(sum + i);
 #pragma unroll 8
         for (int z = 1; z < splits; ++z) v += *reinterpret_cast<const floatx4*>(sum + z * count + i);
         const int64_t m = i / N;
+        const float f = own ? grad_unscale(own[m]) : call;
         *reinterpret_cast<uint2*>(out + m * ldo + (i - m * N)) =
             make_uint2(f32_to_tile<DT>(v[0] * f) | (uint32_t)f32_to_tile<DT>(v[1] * f) << 16,
                        f32_to_tile<DT>(v[2] * f) | (uint32_t)f32_to_tile<DT>(v[3] * f) << 16);
@@ -459,9 +466,9 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const float* sum, int sp
 
 template <int DT>
 hipError_t launch_split_sum(const float* sum, int splits, int64_t M, int N, uint16_t* out, int64_t ldo,
-                            const float* peak, hipStream_t st) {
+                            const float* peak, const float* own, hipStream_t st) {
     const int64_t blocks = (M * N + 1023) / 1024;
-    split_sum_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, peak);
+    split_sum_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, peak, own);
     return hipGetLastError();
 }
 

@@ -19,9 +19,10 @@ struct aq_loss {
     float2* d_seg;         // distillation of few rows: [row][segment] maximum and sum of exponentials
     float* d_list;         // and [row][top] the listed tokens' logits
     float2* d_part;        // [vocabulary tile of 128][max_tokens] maximum and sum of exponentials
-    float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight}, then the peak
+    float* d_row;          // [max_tokens] x {target logit, maximum, log2 of the sum, row weight, peak}, then the call's peak
     // gradient workspace, allocated by the first call that needs it
     uint16_t* d_dlt;       // [piece][tokens] logits' gradient of a piece
+    uint16_t* d_dlx;       // the same scaled token by token (fp16, for dX beside dW)
     uint16_t* d_xt;        // [features][tokens] inputs, transposed
     float* d_dx;           // [split][tokens][features] input gradient of the pieces so far
     size_t dx_bytes;
@@ -370,7 +371,8 @@ struct RowState {          // arrays of n tokens each
     float* ls;             // log2 of the sum of exponentials above it
     float* w;              // row weight of the gradient, 0 for a token that does not count
     float* loss;
-    float* peak;           // the largest entry of the logits' gradient at a target
+    float* own;            // each token's entry of the logits' gradient at its target
+    float* peak;           // the largest of them
 };
 
 // D rows are vocabulary rows, D columns tokens: a lane's values all belong to
@@ -455,46 +457,60 @@ __device__ __forceinline__ float row_weight(const RowState& rs, int64_t t) {
 // groups.  Neighbouring lanes hold neighbouring tokens: each pair of lanes swaps
 // half of its values, so that every store carries two tokens of a row.  4096 x
 // 4096 x 131072 bf16: 3.57 ms, 1.23 PFLOP/s, products, exponentials and stores.
-template <int DT, int WM, int WN, int AM, int AN>
+enum GradScale {
+    GRAD_CALL = 1,         // scaled by the call's peak
+    GRAD_OWN = 2,          // by each token's own
+    GRAD_BOTH = 3
+};
+template <int DT, int SCALE, int WM, int WN, int AM, int AN>
 struct GradEpilogue {
-    uint16_t* dlt;         // [piece][np]
+    uint16_t* dlt;         // [piece][np] (GRAD_CALL)
+    uint16_t* dlx;         // and by tokens (GRAD_OWN)
     int piece, np;
     int64_t v0;            // first vocabulary row of the piece
     RowState rs;
     __device__ void operator()(const floatx16 (&acc)[AM][AN], int, int, int m0, int n0, int M, int N, uint8_t*) const {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int wm = wave / WN, wn = wave - wm * WN, l32 = lane & 31, hi = lane >> 5;
-        const float scale = grad_scale(*rs.peak);
+        const float scale = SCALE & GRAD_CALL ? grad_scale(*rs.peak) : 1.0f;
         const bool odd = lane & 1;
         // the tile's rows from its corner: at most 255 pitches of kMaxPitch
         const __amdgpu_buffer_rsrc_t ro = buffer_rsrc(dlt + (int64_t)m0 * np + n0, kOutOfRange);
+        const __amdgpu_buffer_rsrc_t rx = buffer_rsrc(dlx + (int64_t)m0 * np + n0, kOutOfRange);
 #pragma unroll
         for (int b = 0; b < AN; ++b) {
             const int col = wn * AN * 32 + b * 32 + l32, t = n0 + col;
             const int64_t tv = t < N ? rs.targets[t] - v0 : -1;
             const int target = tv >= 0 && tv < M ? (int)tv - m0 : -1;
             const float top = t < N ? rs.top[t] : 0.0f, ls = t < N ? rs.ls[t] : 0.0f;
-            const float w = t < N ? rs.w[t] * scale : 0.0f;
-            const uint32_t live = w != 0.0f ? 0xffffu : 0u;            // (zeros whatever the logits are)
+            const float w0 = t < N ? rs.w[t] : 0.0f, wc = w0 * scale;
+            const float wo = SCALE & GRAD_OWN ? w0 * (t < N ? grad_scale(rs.own[t]) : 1.0f) : 0.0f;
+            const uint32_t live = w0 != 0.0f ? 0xffffu : 0u;           // (zeros whatever the logits are)
 #pragma unroll
             for (int a = 0; a < AM; ++a)
 #pragma unroll
                 for (int r = 0; r < 16; r += 2) {
                     const int v = (wm * AM + a) * 32 + gemm_row(r, hi);        // rows v and v + 1
-                    uint32_t o[2];
+                    float p[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float p = exp2_fast(__builtin_fmaf(acc[a][b][r + e] - top, kLog2e, -ls));
-                        if (v + e == target) p -= 1.0f;
-                        o[e] = f32_to_tile<DT>(m0 + v + e < M ? p * w : 0.0f) & live;
+                        p[e] = exp2_fast(__builtin_fmaf(acc[a][b][r + e] - top, kLog2e, -ls));
+                        if (v + e == target) p[e] -= 1.0f;
                     }
                     // even lanes keep row v of both tokens, odd lanes row v + 1
-                    const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? o[0] : o[1]), 0xB1, 0xF, 0xF, true);
-                    const uint32_t two = odd ? got | o[1] << 16 : o[0] | got << 16;
                     const int row = v + (odd ? 1 : 0);
                     const bool in = (t & ~1) < np && m0 + row < piece;
-                    __builtin_amdgcn_raw_buffer_store_b32(
-                        two, ro, in ? (uint32_t)(row * np + (col & ~1)) * 2u : kOutOfRange, 0, 0);
+                    const uint32_t off = in ? (uint32_t)(row * np + (col & ~1)) * 2u : kOutOfRange;
+                    auto put = [&](__amdgpu_buffer_rsrc_t to, float w) {
+                        uint32_t o[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) o[e] = f32_to_tile<DT>(m0 + v + e < M ? p[e] * w : 0.0f) & live;
+                        const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? o[0] : o[1]), 0xB1, 0xF, 0xF, true);
+                        const uint32_t two = odd ? got | o[1] << 16 : o[0] | got << 16;
+                        __builtin_amdgcn_raw_buffer_store_b32(two, to, off, 0, 0);
+                    };
+                    if constexpr ((SCALE & GRAD_CALL) != 0) put(ro, wc);
+                    if constexpr ((SCALE & GRAD_OWN) != 0) put(rx, wo);
                 }
         }
     }
@@ -574,6 +590,7 @@ __device__ __forceinline__ void join_tokens(const RowState& rs, const float2* pa
         rs.top[t] = m;
         rs.ls[t] = ls;
         rs.w[t] = w;
+        rs.own[t] = peak;
     }
 #pragma unroll
     for (int o = 1; o < TOK; o <<= 1) peak = fmaxf(peak, __shfl_xor(peak, o));
@@ -603,6 +620,14 @@ int round_up(int64_t v, int to) { return (int)((v + to - 1) / to * to); }
 
 }  // namespace
 
+template <int DT, int SCALE>
+static hipError_t launch_grad(const GemmOperands& g, uint16_t* dlt, uint16_t* dlx, int piece, int np, int64_t v0,
+                              const RowState& rs, hipStream_t st) {
+    const GemmPlan p = gemm_plan(g.M, g.N, g.K, 0);
+    return p.big ? launch_gemm<DT, 2, 4, 4, 2, false>(g, p, GradEpilogue<DT, SCALE, 2, 4, 4, 2>{dlt, dlx, piece, np, v0, rs}, st)
+                 : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, GradEpilogue<DT, SCALE, 2, 2, 2, 2>{dlt, dlx, piece, np, v0, rs}, st);
+}
+
 template <int DT>
 static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W, const RowState& rs, uint16_t* dX,
                                 uint16_t* dW, int n, hipStream_t st) {
@@ -628,32 +653,36 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
                : launch_join<4>(rs, L->d_part, (V + side - 1) / side, n, V, tx, st);
     if (e != hipSuccess || (!dX && !dW)) return e;
     const GemmPlan px = gemm_plan(n, F, std::min(V, piece), L->dx_bytes);
+    const float* own = own_peaks(DT) ? rs.own : nullptr;
+    uint16_t* dlx = own_peaks(DT) && dW ? L->d_dlx : L->d_dlt;       // dX's operand
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
         const int rows = (int)std::min<int64_t>(piece, V - v0);
         const bool first = v0 == 0, last = v0 + piece >= V;
         g.A = W + v0 * F;
         g.M = rows;
-        p = gemm_plan(rows, n, F, 0);
-        e = p.big ? launch_gemm<DT, 2, 4, 4, 2, false>(g, p, GradEpilogue<DT, 2, 4, 4, 2>{L->d_dlt, piece, np, v0, rs}, st)
-                  : launch_gemm<DT, 2, 2, 2, 2, false>(g, p, GradEpilogue<DT, 2, 2, 2, 2>{L->d_dlt, piece, np, v0, rs}, st);
+        if constexpr (own_peaks(DT))
+            e = !dW   ? launch_grad<DT, GRAD_OWN>(g, nullptr, dlx, piece, np, v0, rs, st)
+                : !dX ? launch_grad<DT, GRAD_CALL>(g, L->d_dlt, nullptr, piece, np, v0, rs, st)
+                      : launch_grad<DT, GRAD_BOTH>(g, L->d_dlt, dlx, piece, np, v0, rs, st);
+        else e = launch_grad<DT, GRAD_CALL>(g, L->d_dlt, nullptr, piece, np, v0, rs, st);
         if (e != hipSuccess) return e;
         if (dX) {
             // the sum runs over rows of both operands; dX adds up over the pieces, and over the splits of each
             GemmOperands d = g;
-            d.A = L->d_dlt;
+            d.A = dlx;
             d.lda = np;
             d.M = n;
             d.B = W + v0 * F;
             d.N = F;
             d.K = rows;
             const bool whole = px.splits == 1 && last;
-            const StoreArgs<DT> s{dX, L->d_dx, F, rs.peak};
+            const StoreArgs<DT> s{dX, L->d_dx, F, rs.peak, own};
             e = whole ? (first ? launch_store_gemm<DT, true, STORE_OUT>(d, px, s, st)
                                : launch_store_gemm<DT, true, STORE_LAST>(d, px, s, st))
                       : (first ? launch_store_gemm<DT, true, STORE_SUM>(d, px, s, st)
                                : launch_store_gemm<DT, true, STORE_ADD>(d, px, s, st));
             if (e == hipSuccess && last && !whole)
-                e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.peak, st);
+                e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.peak, own, st);
             if (e != hipSuccess) return e;
         }
         if (dW) {
@@ -665,7 +694,7 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
             d.N = F;
             d.K = np;
             e = launch_store_gemm<DT, false, STORE_OUT>(d, gemm_plan(rows, F, np, 0),
-                                                        StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.peak}, st);
+                                                        StoreArgs<DT>{dW + v0 * F, nullptr, F, rs.peak, nullptr}, st);
             if (e != hipSuccess) return e;
         }
     }
@@ -696,7 +725,7 @@ static hipError_t distill(DistillArgs a, hipStream_t st) {
 namespace {
 
 void free_loss(aq_loss* L) {
-    void* ptrs[] = {L->d_seg, L->d_list, L->d_zero, L->d_part, L->d_row, L->d_dlt, L->d_xt, L->d_dx};
+    void* ptrs[] = {L->d_seg, L->d_list, L->d_zero, L->d_part, L->d_row, L->d_dlt, L->d_dlx, L->d_xt, L->d_dx};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     delete L;
@@ -715,12 +744,15 @@ constexpr size_t kSplitBytes = size_t(64) << 20;   // most that a K split's sums
 
 // The gradients' workspace (the first call that asks for one allocates it).
 aq_status grad_workspace(aq_loss* L, bool dx, bool dw, void* stream) {
-    if (L->d_dlt && (!dx || L->d_dx) && (!dw || L->d_xt)) return AQ_OK;
+    // (from the call on that makes it both gradients' handle, whether or not one call asks for both)
+    const bool two = (dx || L->d_dx) && (dw || L->d_xt) && aq::own_peaks(L->desc.dtype);
+    if (L->d_dlt && (!dx || L->d_dx) && (!dw || L->d_xt) && (!two || L->d_dlx)) return AQ_OK;
     if (aq::capturing(static_cast<hipStream_t>(stream)))
         return api_fail(AQ_ERR_UNSUPPORTED, "the first call with a gradient allocates: not under graph capture");
     const size_t n = (size_t)(L->desc.max_tokens + 7) / 8 * 8, F = (size_t)L->desc.features, P = (size_t)L->piece;
     aq_status s = AQ_OK;
     s = alloc(&L->d_dlt, n * P * 2, "gradient workspace");
+    if (s == AQ_OK && two) s = alloc(&L->d_dlx, n * P * 2, "gradient workspace");
     if (s == AQ_OK && dx && !L->d_dx) {
         const int64_t mt = L->desc.max_tokens;
         const size_t split = aq::gemm_split_bytes(mt, F, std::min<int64_t>(L->desc.vocab, L->piece), kSplitBytes);
@@ -790,7 +822,7 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out) {
         const size_t n = (size_t)desc->max_tokens, tiles = (size_t)(desc->vocab + 127) / 128;
         s = alloc(&L->d_zero, 256, "zero block");
         if (s == AQ_OK) s = alloc(&L->d_part, tiles * n * sizeof(float2), "row statistics");
-        if (s == AQ_OK) s = alloc(&L->d_row, (4 * n + 1) * sizeof(float), "row state");
+        if (s == AQ_OK) s = alloc(&L->d_row, (5 * n + 1) * sizeof(float), "row state");
         if (s == AQ_OK && (e = hipMemset(L->d_zero, 0, 256)) != hipSuccess) s = api_hip_fail(e, "zero block");
         if (s == AQ_OK && (e = hipDeviceSynchronize()) != hipSuccess) s = api_hip_fail(e, "zero block");
     }
@@ -825,7 +857,7 @@ aq_status aq_loss_cross_entropy(aq_loss* L, const void* X, const void* W, const 
     }
     const int64_t mt = L->desc.max_tokens;
     const aq::RowState rs{targets, dloss, L->d_row, L->d_row + mt, L->d_row + 2 * mt, L->d_row + 3 * mt, loss,
-                          L->d_row + 4 * mt};
+                          L->d_row + 4 * mt, L->d_row + 5 * mt};
     const auto st = static_cast<hipStream_t>(stream);
     const auto x = static_cast<const uint16_t*>(X), w = static_cast<const uint16_t*>(W);
     const auto dx = static_cast<uint16_t*>(dX), dw = static_cast<uint16_t*>(dW);

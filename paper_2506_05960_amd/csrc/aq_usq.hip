@@ -899,7 +899,7 @@ hipError_t launch_few_grad(const UsqArgs& a, const uint16_t* dy, int cp, float* 
     else if (a.n <= 32) usq_few_grad_kernel<DT, SG, 2><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
     else usq_few_grad_kernel<DT, SG, 4><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_split_sum<DT>(sum, splits, a.n, a.K, dX, a.K, nullptr, st);
+    return e != hipSuccess ? e : launch_split_sum<DT>(sum, splits, a.n, a.K, dX, a.K, nullptr, nullptr, st);
 }
 
 // dst[r][c] of pitch cp = src[r][c], zero for C <= c < cp.
@@ -941,12 +941,12 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
         if ((e = hipGetLastError()) != hipSuccess) return e;
         g.N = cols;
         const GemmPlan p = gemm_plan(n, cols, cp, L->dsum_bytes);
-        const StoreArgs<DT> s{dX + k0, L->d_dsum, K, nullptr};
+        const StoreArgs<DT> s{dX + k0, L->d_dsum, K, nullptr, nullptr};
         e = p.splits > 1 ? launch_store_gemm<DT, false, STORE_SUM>(g, p, s, st)
                          : launch_store_gemm<DT, false, STORE_OUT>(g, p, s, st);
         if (e != hipSuccess) return e;
         if (p.splits > 1 &&
-            (e = launch_split_sum<DT>(L->d_dsum, p.splits, n, cols, dX + k0, K, nullptr, st)) != hipSuccess)
+            (e = launch_split_sum<DT>(L->d_dsum, p.splits, n, cols, dX + k0, K, nullptr, nullptr, st)) != hipSuccess)
             return e;
     }
     return hipSuccess;

@@ -43,3 +43,35 @@ def test_distill_lists_a_token_masked_by_the_lowest_value(dtype, vocab, T):
     assert TL.within(loss, want, want.abs() * 2.0 ** -17)
     b = T * (q + P) * 2.0 ** -16
     assert TL.within(grad, want_grad, b + TL.half_step(want_grad.abs() + b, dtype))
+
+
+@pytest.mark.parametrize("both", [True, False])
+@pytest.mark.parametrize("n,V", [(40, 30011), (200, 2003)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_cross_entropy_rows_of_far_smaller_weights(dtype, n, V, both):
+    """Weights from 2^12 down to 2^-12 in one call: each row of dX against its own bound.
+
+    A row's stored dz is rounded once: half a step, at least half the smallest subnormal step (2^-25 in fp16) under the
+    scale that takes the row's entry at its target to 32640 (just below 2^15: 2^-39 of that entry).  p and the sums as in
+    test_gpu_losses.py.  The head's weights are positive, so that errors of one sign add up."""
+    F = 64
+    x, w, targets, _ = TL.ce_inputs(n, F, V, dtype, 31)
+    w = w.abs()
+    dloss = 2.0 ** torch.linspace(12, -12, n).round().cuda()
+    L = TL.losses(V, F, dtype, n)
+    loss, dx, dw = L.cross_entropy(x, w, targets, dloss, dx=True, dw=both)
+    TL.check_ce(x, w, targets, dloss, dtype, loss, None, dw)
+    x, w, counts = x.double(), w.double(), targets >= 0
+    z = x @ w.t()
+    p = torch.softmax(z, dim=1)
+    dz = p.clone()
+    rows = torch.arange(n, device="cuda")[counts]
+    dz[rows, targets[counts]] -= 1
+    weight = (dloss.double() * counts)[:, None]
+    rel = TL.U * (2 * 1.4427 * z.abs().amax(dim=1) + 4 + V / 256 + 300)[:, None]
+    peak = torch.zeros(n, 1, dtype=torch.float64, device="cuda")
+    peak[rows, 0] = dz[rows, targets[counts]].abs().clamp(min=2.0 ** -20)        # (less is rounding)
+    eps = torch.finfo(DT[dtype]).eps
+    ddz = weight * (dz.abs() * (eps / 2) + 2 * (p + (dz - p).abs()) * rel + peak * 2.0 ** -39)
+    want, b = (weight * dz) @ w, ddz @ w + (V + 64) * TL.U * ((weight * dz).abs() @ w)
+    assert TL.within(dx, want, b + TL.half_step(want.abs() + b, dtype))
