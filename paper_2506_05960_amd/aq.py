@@ -576,10 +576,11 @@ def _ptr(t):
 
 
 def _int32(**values) -> None:
-    """Refuse what a descriptor's 32-bit fields would wrap."""
+    """Refuse what a descriptor's 32-bit fields (64 bits: max_tokens) would wrap."""
     for name, v in values.items():
-        if v >= 1 << 31:
-            raise ValueError(f"{name} is past 2^31 - 1")
+        bits = 63 if name == "max_tokens" else 31
+        if not -(1 << bits) <= v < 1 << bits:
+            raise ValueError(f"{name} is past {'-' if v < 0 else ''}2^{bits}{'' if v < 0 else ' - 1'}")
 
 
 class USQLayer:
@@ -604,7 +605,7 @@ class USQLayer:
         if len(shape) != 2 or min(shape) < 1:
             raise ValueError(f"codes must be a matrix, got shape {shape}")
         self.C_out, self.K = shape[0], 2 * shape[1]
-        _int32(group=group, C_out=self.C_out, K=self.K)
+        _int32(group=group, C_out=self.C_out, K=self.K, max_tokens=max_tokens)
         G = -(-self.K // group)
         codes = _host_array("codes", codes, torch.uint8, (self.C_out, self.K // 2))
         scales = _host_array("scales", scales, _torch_dtype(dtype), (self.C_out, G))
@@ -662,7 +663,7 @@ class VocabLoss:
             raise ValueError("dtype must be f16, bf16 or f32")
         if features is not None and features < 1:
             raise ValueError("features must be a positive int or None")
-        _int32(vocab=vocab, features=features or 0)
+        _int32(vocab=vocab, features=features or 0, max_tokens=max_tokens)
         self.vocab, self.features, self.dtype, self.max_tokens = vocab, features, dtype, max_tokens
         self.device = torch.cuda.current_device() if torch.cuda.is_available() else None
         self.handle = aq_loss_create(aq_loss_desc(vocab, features or 0, DTYPE_CODES[dtype], max_tokens))

@@ -79,3 +79,14 @@ def test_temperatures_without_a_finite_reciprocal_are_refused(so):
     """log2(e) / T scales the logits: an infinity makes NaN of every row's largest logit."""
     got = host_device.in_child(so, "test_usq_losses_workspace_host", "temperatures", [2.0 ** -149, 2.0 ** -128, 2.0 ** -127, 1e30])
     assert got == [A.AQ_ERR_UNSUPPORTED, A.AQ_ERR_UNSUPPORTED, A.AQ_OK, A.AQ_OK]
+
+
+def test_descriptors_refuse_what_would_wrap_from_below_or_in_64_bits():
+    codes, scales = np.zeros((24, 32), np.uint8), np.ones((24, 2), np.float16)
+    with pytest.raises(ValueError, match="vocab is past -2\\^31"):
+        A.VocabLoss(5 - (1 << 32), max_tokens=2)
+    for most in ((1 << 64) + 4, 4 - (1 << 64)):
+        with pytest.raises(ValueError, match="max_tokens is past -?2\\^63"):
+            A.VocabLoss(5, max_tokens=most)
+        with pytest.raises(ValueError, match="max_tokens is past -?2\\^63"):
+            A.USQLayer(codes, scales, group=32, max_tokens=most)
