@@ -339,32 +339,41 @@ hipError_t launch_few(const UsqArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Output rows a workgroup (16 RT): more of them share the tokens' reads, fewer fill the chip.  us, RT = 1 / 2 / 4:
-//   4096 -> 16384:   1 token  9.2 / 7.3 / 7.7    16 tokens 11.9 / 9.5 / 9.8    32: 21.6 / 15.8 / 13.0
-//                   64 tokens 43.4 / 28.1 / 20.7
-//   4096 -> 4096:    1 token  5.9 / 5.7 / 6.8    32 tokens 7.3 / 7.6 / 9.4     64: 12.2 / 11.2 / 14.7
-//   16384 -> 4096:   1 token 10.5 / 13.3 / 20.8  16 tokens 13.1 / 16.8 / 25.3  64: 38.4 / 36.2 / 49.6
-// Long reductions in few row tiles take sixteen waves: 16384 -> 4096, 1 token 10.5 -> 9.1, 16 tokens 13.1 -> 12.4.
+// Output rows a workgroup (16 RT).  Compute units that take a second workgroup take twice the time, so two row tiles
+// share a workgroup, and the tokens' reads, where there are more than 256 of them, and four where there are more than
+// 512 (groups of 128 and more: finer ones have too many values to hold for 64 tokens).  us, RT = 1 / 2 / 4, row tiles
+// in front:
+//   K 4096, group 128, 24 tokens:  256  6.2 / 6.9 / 9.2    288  8.5 / 7.0 / 9.1     512  9.3 / 8.2 / 10.6    576 11.1 / 11.3 / 10.6
+//                      64 tokens:  256 11.2 / 10.6 / 14.3  288 17.8 / 10.9 / 14.4   512 20.8 / 14.0 / 16.3   576 27.1 / 22.1 / 16.4
+//   K 2304, group 32,  24 tokens:  256  5.8 / 6.7 / 9.9    288  7.3 / 6.7 / 9.9     512  8.2 / 7.2 / 10.1    576 10.9 / 11.7 / 10.1
+//                      48 tokens:  256  8.8 / 9.7          288 14.9 / 9.9           512 16.5 / 10.9          576 22.0 / 18.9
+// Up to 16 tokens two tiles at most, and short reductions not before there are more than 768 of them:
+//   K 8192, 1 token:   256 6.4 / 7.6    288 8.6 / 7.7    576 11.5 / 11.1    1024 15.2 / 12.8
+//   K 4096, 1 token:   256 4.9 / 4.9    288 5.3 / 4.9    448  5.6 / 5.1     1024  9.0 / 7.2
+//   K 2304, 1 token:   288 5.1 / 5.4    576 5.2 / 5.5    768  5.3 / 5.4      896  6.5 / 5.6
+// Long reductions in up to 256 row tiles take sixteen waves: K 8192, 1 token, 128 tiles 5.7 -> 5.3, 256 6.4 -> 5.7.
 template <int DT, int SG>
 hipError_t launch_few(const UsqArgs& a, hipStream_t st) {
+    constexpr int kUnits = 256;
     const int tiles = (a.C_out + 15) / 16;
+    const bool one = tiles <= kUnits, two = tiles <= 2 * kUnits;
     if (a.n <= 16) {
-        const bool long_few = tiles < 512 && a.nchunk >= 64;
+        const bool wide = (!one && a.nchunk >= 32) || tiles > 3 * kUnits, deep = one && a.nchunk >= 64;
         if (a.n <= 4)
-            return tiles >= 512 ? launch_few<DT, SG, 1, 2, 2, 8, false>(a, st)
-                   : long_few   ? launch_few<DT, SG, 1, 1, 2, 16, false>(a, st)
-                                : launch_few<DT, SG, 1, 1, 2, 8, false>(a, st);
-        return tiles >= 512 ? launch_few<DT, SG, 1, 2, 1, 8, true>(a, st)
-               : long_few   ? launch_few<DT, SG, 1, 1, 1, 16, true>(a, st)
-                            : launch_few<DT, SG, 1, 1, 1, 8, true>(a, st);
+            return wide   ? launch_few<DT, SG, 1, 2, 2, 8, false>(a, st)
+                   : deep ? launch_few<DT, SG, 1, 1, 2, 16, false>(a, st)
+                          : launch_few<DT, SG, 1, 1, 2, 8, false>(a, st);
+        return wide   ? launch_few<DT, SG, 1, 2, 1, 8, true>(a, st)
+               : deep ? launch_few<DT, SG, 1, 1, 1, 16, true>(a, st)
+                      : launch_few<DT, SG, 1, 1, 1, 8, true>(a, st);
     }
     if (a.n <= 32)
-        return tiles >= 1024  ? launch_few<DT, SG, 2, 4, 1, 8, true>(a, st)
-               : tiles >= 300 ? launch_few<DT, SG, 2, 2, 1, 8, true>(a, st)
-                              : launch_few<DT, SG, 2, 1, 1, 8, true>(a, st);
-    if constexpr (SG == 4)      // (groups below 128 have too many values to hold)
-        if (tiles >= 768) return launch_few<DT, SG, 4, 4, 1, 8, true>(a, st);
-    return tiles >= 256 ? launch_few<DT, SG, 4, 2, 1, 8, true>(a, st) : launch_few<DT, SG, 4, 1, 1, 8, true>(a, st);
+        return one   ? launch_few<DT, SG, 2, 1, 1, 8, true>(a, st)
+               : two ? launch_few<DT, SG, 2, 2, 1, 8, true>(a, st)
+                     : launch_few<DT, SG, 2, 4, 1, 8, true>(a, st);
+    if constexpr (SG == 4)
+        if (!two) return launch_few<DT, SG, 4, 4, 1, 8, true>(a, st);
+    return one ? launch_few<DT, SG, 4, 1, 1, 8, true>(a, st) : launch_few<DT, SG, 4, 2, 1, 8, true>(a, st);
 }
 
 // ---- many tokens ----

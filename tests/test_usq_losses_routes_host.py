@@ -1,0 +1,53 @@
+"""Which kernels calls of the 4-bit layers and the vocabulary losses take, by their launches' shapes (no GPU needed).
+
+The GPU tests of these routes (``test_gpu_operator_routes.py``) take their sizes from here, so that a change of the
+plans that leaves a variant without a test shows."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import host_device
+from paper_2506_05960_amd import aq as A
+
+# few tokens: n, K, C_out, output rows a workgroup takes (16 a row tile), waves
+FEW_ROUTES = [
+    (1, 264, 4096, 16, 3), (4, 264, 12288, 16, 3), (1, 264, 12305, 32, 3), (1, 4104, 4096, 16, 8), (4, 4104, 4101, 32, 8),
+    (5, 264, 12288, 16, 3), (16, 264, 12305, 32, 3), (16, 4104, 4096, 16, 8), (5, 4104, 4101, 32, 8),
+    (17, 264, 4096, 16, 3), (32, 264, 4101, 32, 3), (17, 264, 8192, 32, 3), (32, 264, 8209, 64, 3),
+    (33, 264, 4096, 16, 3), (64, 264, 4101, 32, 3), (33, 264, 8192, 32, 3), (64, 264, 8209, 64, 3),
+    (3, 8200, 300, 16, 16), (9, 8200, 300, 16, 16), (1, 8200, 4101, 32, 8), (16, 8200, 4101, 32, 8), (64, 8200, 300, 16, 8),
+]
+
+
+def _usq(n, K, C_out, group=128, call="aq_usq_forward"):
+    """Grid and block of each launch of a layer's second call over n tokens."""
+    lib, h = A.load_library(), ctypes.c_void_p()
+    d = A.aq_usq_desc(C_out, K, group, A.AQ_BF16, A.AQ_BF16, n)
+    codes, scales = np.zeros((C_out, K // 2), np.uint8), np.zeros((C_out, -(-K // group)), np.uint16)
+    assert lib.aq_usq_create(ctypes.byref(d), codes.ctypes.data, scales.ctypes.data, None, ctypes.byref(h)) == A.AQ_OK
+    f = getattr(lib, call)
+    assert f(h, 4096, 4096, n, None) == A.AQ_OK
+    st, out = host_device.launches(lambda: f(h, 4096, 4096, n, None))
+    assert st == A.AQ_OK
+    lib.aq_usq_destroy(h)
+    return [(x, y, b) for x, y, _, b, *_ in out]
+
+
+def few(routes, group):
+    return [_usq(n, K, C_out, group) for n, K, C_out, *_ in routes]
+
+
+@pytest.fixture(scope="module")
+def so(tmp_path_factory):
+    A.load_library()
+    return host_device.build(tmp_path_factory)
+
+
+@pytest.mark.parametrize("group", [64, 128])
+def test_few_token_routes(so, group):
+    for route, got in zip(FEW_ROUTES, host_device.in_child(so, "test_usq_losses_routes_host", "few", FEW_ROUTES, group)):
+        n, K, C_out, rows, waves = route
+        if n > 32 and group < 128:
+            rows = min(rows, 32)
+        assert got == [[-(-C_out // rows), 1, 64 * waves]], route
