@@ -511,7 +511,7 @@ aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void*
  *            may be `logits` itself; NULL: not computed
  *   n        1 <= n <= max_tokens
  * Asynchronous, allocates nothing; sums are fp32 in a fixed order for each n.
- * Calls of up to 256 tokens use the handle's workspace: serialise them on one
+ * Calls of up to 192 tokens use the handle's workspace: serialise them on one
  * stream.
  */
 aq_status aq_loss_distill(aq_loss* loss_handle, const void* logits, const int32_t* ids, const void* teacher,

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(THREADS, 4) distill_kernel(DistillArgs a) {
 
 // Few long rows, in segments: a launch for the statistics, and one that joins them and writes the gradient.  One
 // workgroup a row is bound by what a compute unit loads and exponentiates.
-constexpr int kMaxSegments = 1024, kMaxSegmentRows = 256;
+constexpr int kMaxSegments = 1024, kMaxSegmentRows = 192;
 template <int DT, DistillPart PART>
 __global__ void __launch_bounds__(256, 4) distill_segment_kernel(DistillArgs a) {
     const int row = (int)blockIdx.y;
@@ -701,23 +701,32 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
     return hipSuccess;
 }
 
-// Up to 256 rows of 64 KB and more in segments, whole rows against segments: bf16, 1 x 131072 30.9 / 10.7 us,
-// 16 x 131072 31.5 / 12.0, 200 x 131072 40.5 / 36.0, 16 x 32768 10.9 / 9.9, 200 x 32768 18.2 / 15.6; of 16 KB
-// the second launch costs as much as it gives: 1 x 8000 7.6 / 9.9, 64 x 8000 13.9 / 12.5.
-static bool distill_segmented(int64_t n, int64_t V, int vec) { return n <= kMaxSegmentRows && V / vec >= 4096; }
+// Rows in segments: as many as leave half of the compute units without one, of 32768 values and more (what a workgroup
+// exponentiates bounds it, so values count, not bytes), and up to three quarters of that many, three times as long.  us,
+// whole rows / segments, fp32 and bf16:
+//   1 row    24579 values  9.4 / 9.4, 10.5 / 9.6    32771 10.7 / 10.0, 11.5 / 9.3      131075 30.5 / 9.2, 27.4 / 9.4
+//   64 rows  24579        11.1 / 11.5, 11.4 / 11.4  32771 13.1 / 11.7, 12.4 / 11.6     131075 32.7 / 19.8, 28.6 / 14.3
+//   128      24579        11.8 / 12.7, 12.0 / 12.3  32771 13.9 / 13.6, 12.7 / 12.3     131075 53.7 / 39.2, 29.2 / 21.3
+//   160      65539        24.2 / 26.1, 19.7 / 17.3  98307 42.6 / 37.7, 24.1 / 21.0     131075 55.7 / 47.1, 30.7 / 27.9
+//   200      65539        31.9 / 32.3, 19.9 / 19.7  98307 45.7 / 45.6, 24.7 / 26.4     131075 59.4 / 56.2, 36.2 / 34.0
+//   256      65539        35.9 / 39.6, 20.2 / 21.8  98307 52.5 / 53.5, 28.9 / 32.6     131075 67.5 / 67.9, 39.2 / 41.3
+static bool distill_segmented(int64_t n, int64_t V) { return n <= 128 ? V >= 32768 : n <= kMaxSegmentRows && V >= 98304; }
 
 template <int DT>
 static hipError_t distill(DistillArgs a, hipStream_t st) {
     const int64_t vecs = a.V / Store<DT>::kVec;
-    if (distill_segmented(a.n, a.V, Store<DT>::kVec)) {
+    if (distill_segmented(a.n, a.V)) {
         a.segs = (int)std::min<int64_t>(64, kMaxSegments / a.n);
         a.seg_vecs = (int)((vecs + a.segs - 1) / a.segs);
         return launch_distill_segments<DT>(a, st);
     }
-    // Rows of up to some 100 KB at four workgroups a compute unit, longer ones and few rows with more threads a row:
-    // 4096 x 32768 bf16 122 against 159 us, 1024 x 49999 fp16 50 against 53; 4096 x 131072 bf16 551 against 513.
-    return a.n >= 512 && (int64_t)a.V * (16 / Store<DT>::kVec) <= 100000 ? launch_distill<DT, 256, 16>(a, st)
-                                                                        : launch_distill<DT, 512, 14>(a, st);
+    // More rows than the 512 that larger workgroups hold at a time (two a compute unit) go to smaller ones (four), up to
+    // the length where reading again what those do not hold costs more: us, smaller / larger, 4096 rows of 96, 108, 112
+    // and 128 KB, bf16 169 / 177, 187 / 193, 203 / 200, 250 / 224, fp16 164 / 175, 184 / 193, 199 / 199, 246 / 222; fp32,
+    // 48, 60, 64 and 68 KB, 82 / 91, 102 / 103, 115 / 114, 116 / 112.  1024 rows, 64 KB, bf16 29.9 / 33.6; 600, 92 KB,
+    // 32.8 / 32.9; 512, 64 KB, 19.6 / 18.2.
+    return a.n > 512 && vecs <= (DT == AQ_F32 ? 4096 : 7168) ? launch_distill<DT, 256, 16>(a, st)
+                                                             : launch_distill<DT, 512, 14>(a, st);
 }
 
 }  // namespace aq
@@ -882,7 +891,7 @@ aq_status aq_loss_distill(aq_loss* L, const void* logits, const int32_t* ids, co
     const aq_status s = check_call(L, n);
     if (s != AQ_OK) return s;
     if (overlaps(loss, dloss, n) &&
-        (loss != dloss || aq::distill_segmented(n, L->desc.vocab, L->desc.dtype == AQ_F32 ? 4 : 8)))
+        (loss != dloss || aq::distill_segmented(n, L->desc.vocab)))
         return api_fail(AQ_ERR_INVALID_ARGUMENT, "loss overlaps dloss");
     const aq::DistillArgs a{logits, ids, teacher, dloss, loss, dlogits, n, L->desc.vocab, top, aq::kLog2e / temperature,
                             temperature, 0, 0, L->d_seg, L->d_list};

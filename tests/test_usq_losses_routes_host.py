@@ -19,6 +19,15 @@ FEW_ROUTES = [
     (3, 8200, 300, 16, 16), (9, 8200, 300, 16, 16), (1, 8200, 4101, 32, 8), (16, 8200, 4101, 32, 8), (64, 8200, 300, 16, 8),
 ]
 
+# distillation: n, vocab, dtype, launches, threads of the last one
+DISTILL_ROUTES = [
+    (1, 32767, "f32", 1, 512), (1, 32768, "f32", 2, 256), (128, 32768, "bf16", 2, 256), (129, 32768, "bf16", 1, 512),
+    (129, 98303, "f16", 1, 512), (129, 98304, "f16", 2, 256), (192, 98309, "bf16", 2, 256), (193, 98309, "bf16", 1, 512),
+    (512, 2003, "bf16", 1, 512), (513, 2003, "f32", 1, 256), (513, 2003, "f16", 1, 256), (513, 40003, "bf16", 1, 256),
+    (514, 57351, "f16", 1, 256), (513, 57353, "bf16", 1, 512), (513, 16387, "f32", 1, 256), (513, 17001, "f32", 1, 512),
+    (257, 60001, "f16", 1, 512), (257, 60003, "bf16", 1, 512), (257, 30001, "f32", 1, 512),
+]
+
 
 def _usq(n, K, C_out, group=128, call="aq_usq_forward"):
     """Grid and block of each launch of a layer's second call over n tokens."""
@@ -38,6 +47,18 @@ def few(routes, group):
     return [_usq(n, K, C_out, group) for n, K, C_out, *_ in routes]
 
 
+def distills(routes):
+    lib, out = A.load_library(), []
+    for n, V, dtype, *_ in routes:
+        h = ctypes.c_void_p()
+        assert lib.aq_loss_create(ctypes.byref(A.aq_loss_desc(V, 0, A.DTYPE_CODES[dtype], n)), ctypes.byref(h)) == A.AQ_OK
+        st, got = host_device.launches(lambda: lib.aq_loss_distill(h, 4096, 4096, 4096, 9, 1.0, None, 4096, 4096, n, None))
+        assert st == A.AQ_OK
+        lib.aq_loss_destroy(h)
+        out.append([len(got), got[-1][3]])
+    return out
+
+
 @pytest.fixture(scope="module")
 def so(tmp_path_factory):
     A.load_library()
@@ -51,3 +72,8 @@ def test_few_token_routes(so, group):
         if n > 32 and group < 128:
             rows = min(rows, 32)
         assert got == [[-(-C_out // rows), 1, 64 * waves]], route
+
+
+def test_distillation_routes(so):
+    got = host_device.in_child(so, "test_usq_losses_routes_host", "distills", DISTILL_ROUTES)
+    assert got == [[launches, threads] for *_, launches, threads in DISTILL_ROUTES]
