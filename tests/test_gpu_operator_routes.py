@@ -1,7 +1,7 @@
-"""GPU tests of the 4-bit layers and the distillation at sizes that take every
-kernel variant: wide and long layers of few tokens, many and long rows.  Which
-sizes take which variant is held by the launches' shapes in
-``test_usq_losses_routes_host.py``.
+"""GPU tests of the 4-bit layers and the vocabulary losses at sizes that take
+every kernel variant: large tiles of the dense product, wide and long layers of
+few tokens, many and long rows of the distillation.  Which sizes take which
+variant is held by the launches' shapes in ``test_usq_losses_routes_host.py``.
 
 The bounds are those of ``test_gpu_usq.py`` and ``test_gpu_losses.py``.
 """
@@ -10,7 +10,7 @@ import torch
 
 import test_gpu_losses as TL
 import test_gpu_usq as TU
-from test_usq_losses_routes_host import DISTILL_ROUTES, FEW_ROUTES
+from test_usq_losses_routes_host import CE_ROUTES, DISTILL_ROUTES, FEW_ROUTES, GRAD_ROUTES
 
 pytestmark = pytest.mark.gpu
 
@@ -45,6 +45,52 @@ def test_few_tokens(K, C_out, group, dtype, y):
         bound = bound + TU.half_step(want.abs() + bound, y)
         assert bool(((got - want).abs() <= bound).all()), n
         assert bool((out[n] == 7).all())
+
+
+@pytest.mark.parametrize("dtype,group", [("f16", 32), ("bf16", 64), ("f16", 128), ("bf16", 256)])
+@pytest.mark.parametrize("n,K,C_out", [(1100, 392, 300), (2100, 264, 130), (70, 4104, 520)])
+def test_many_tokens(n, K, C_out, group, dtype):
+    """More than eight tiles of tokens (two bands of them), and K in several splits."""
+    codes, scales, z, W, mag = TU.make(K, C_out, group, dtype, True, seed=n)
+    lay = TU.layer_of(codes, scales, z, group, dtype, "f32", n)
+    x = torch.randn(n, K, generator=torch.Generator().manual_seed(n)).to(DT[dtype]).cuda()
+    out = torch.full((n + 1, C_out), 7.0, device="cuda")
+    got = lay.forward(x, out=out[:n]).double()
+    want = x.double() @ W.t().cuda()
+    bound = (2 * K + 8) * TU.U32 * (x.double().abs() @ mag.t().cuda())
+    assert bool(((got - want).abs() <= bound + TU.half_step(want.abs() + bound, "f32")).all())
+    assert bool((out[n] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,K,C_out", [r[:3] for r in GRAD_ROUTES])
+def test_input_grad(n, K, C_out, dtype):
+    codes, scales, z, W, _ = TU.make(K, C_out, 64, dtype, True, seed=n)
+    lay = TU.layer_of(codes, scales, z, 64, dtype, dtype, n)
+    dy = torch.randn(n, C_out, generator=torch.Generator().manual_seed(n)).to(DT[dtype])
+    out = torch.full((n + 1, K), 7.0, dtype=DT[dtype], device="cuda")
+    got = lay.input_grad(dy.cuda(), out=out[:n]).double()
+    W, d = W.cuda(), dy.double().cuda()
+    want = d @ W
+    bound = d.abs() @ TU.half_step(W, dtype) + (C_out + 8) * TU.U32 * (d.abs() @ W.abs())
+    assert bool(((got - want).abs() <= bound + TU.half_step(want.abs() + bound, dtype)).all())
+    assert bool((out[n] == 7).all())
+
+
+# ---- cross entropy ----
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,F,V,most", [r[:4] for r in CE_ROUTES])
+def test_cross_entropy(n, F, V, most, dtype):
+    x, w, targets, dloss = TL.ce_inputs(n, F, V, dtype, n + V)
+    targets[:4] = torch.tensor([0, V - 1, V - 1, 255])
+    L = TL.losses(V, F, dtype, most)
+    loss, dx, dw = L.cross_entropy(x, w, targets, dloss, dx=True, dw=True)
+    TL.check_ce(x, w, targets, dloss, dtype, loss, dx, dw)
+    again = L.cross_entropy(x, w, targets, dloss, dx=True, dw=True)
+    assert all(torch.equal(a, b) for a, b in zip(again, (loss, dx, dw)))
+    for got in (L.cross_entropy(x, w, targets, dloss, dx=True), L.cross_entropy(x, w, targets, dloss, dw=True)):
+        TL.check_ce(x, w, targets, dloss, dtype, *got)
 
 
 # ---- distillation ----

@@ -10,6 +10,8 @@ import pytest
 import host_device
 from paper_2506_05960_amd import aq as A
 
+BIG, SMALL = 512, 256        # threads of the dense product's 256 x 256 and 128 x 128 tiles
+
 # few tokens: n, K, C_out, output rows a workgroup takes (16 a row tile), waves
 FEW_ROUTES = [
     (1, 264, 4096, 16, 3), (4, 264, 12288, 16, 3), (1, 264, 12305, 32, 3), (1, 4104, 4096, 16, 8), (4, 4104, 4101, 32, 8),
@@ -17,6 +19,21 @@ FEW_ROUTES = [
     (17, 264, 4096, 16, 3), (32, 264, 4101, 32, 3), (17, 264, 8192, 32, 3), (32, 264, 8209, 64, 3),
     (33, 264, 4096, 16, 3), (64, 264, 4101, 32, 3), (33, 264, 8192, 32, 3), (64, 264, 8209, 64, 3),
     (3, 8200, 300, 16, 16), (9, 8200, 300, 16, 16), (1, 8200, 4101, 32, 8), (16, 8200, 4101, 32, 8), (64, 8200, 300, 16, 8),
+]
+
+# input gradients: n, K, C_out, threads of the product's workgroups, its workgroups
+GRAD_ROUTES = [(2100, 4104, 4099, BIG, 9 * 17), (513, 4104, 8195, BIG, 5 * 3 * 17), (300, 4104, 4099, SMALL, 5 * 3 * 33),
+               (1100, 2312, 4099, SMALL, 9 * 19)]
+
+# cross entropy: n, features, vocab, max_tokens; threads of the statistics, and of the gradient, dX and dW products of
+# each piece; K splits of dX; pieces
+CE_ROUTES = [
+    (1030, 136, 9001, 1030, BIG, BIG, SMALL, SMALL, 13, 1),
+    (2100, 4104, 2100, 2100, SMALL, SMALL, BIG, BIG, 1, 1),
+    (130, 4104, 9001, 130, SMALL, SMALL, BIG, BIG, 15, 1),
+    (2100, 4104, 1100, 1 << 17, SMALL, SMALL, BIG, SMALL, 1, 3),
+    (130, 72, 1100, 1 << 18, SMALL, SMALL, SMALL, SMALL, 1, 5),
+    (5, 64, 5001, 1 << 15, SMALL, SMALL, SMALL, SMALL, 28, 3),
 ]
 
 # distillation: n, vocab, dtype, launches, threads of the last one
@@ -45,6 +62,22 @@ def _usq(n, K, C_out, group=128, call="aq_usq_forward"):
 
 def few(routes, group):
     return [_usq(n, K, C_out, group) for n, K, C_out, *_ in routes]
+
+
+def grads(routes):
+    return [_usq(n, K, C_out, 64, "aq_usq_input_grad") for n, K, C_out, *_ in routes]
+
+
+def cross_entropies(routes):
+    lib, out = A.load_library(), []
+    for n, F, V, most, *_ in routes:
+        h = ctypes.c_void_p()
+        assert lib.aq_loss_create(ctypes.byref(A.aq_loss_desc(V, F, A.AQ_BF16, most)), ctypes.byref(h)) == A.AQ_OK
+        st, got = host_device.launches(lambda: lib.aq_loss_cross_entropy(h, 4096, 4096, 4096, None, 4096, 4096, 4096, n, None))
+        assert st == A.AQ_OK
+        lib.aq_loss_destroy(h)
+        out.append([(x, b) for x, _, _, b, *_ in got])
+    return out
 
 
 def distills(routes):
@@ -77,3 +110,26 @@ def test_few_token_routes(so, group):
 def test_distillation_routes(so):
     got = host_device.in_child(so, "test_usq_losses_routes_host", "distills", DISTILL_ROUTES)
     assert got == [[launches, threads] for *_, launches, threads in DISTILL_ROUTES]
+
+
+def test_input_gradient_routes(so):
+    for route, got in zip(GRAD_ROUTES, host_device.in_child(so, "test_usq_losses_routes_host", "grads", GRAD_ROUTES)):
+        n, K, C_out, threads, wgs = route
+        assert [wgs, 1, threads] in got, (route, got)
+
+
+def test_cross_entropy_routes(so):
+    for route, got in zip(CE_ROUTES, host_device.in_child(so, "test_usq_losses_routes_host", "cross_entropies", CE_ROUTES)):
+        n, F, V, most, stats, grad, dx, dw, splits, pieces = route
+        tiles = lambda M, N, threads: -(-M // (128 if threads == SMALL else 256)) * -(-N // (128 if threads == SMALL else 256))
+        assert got[0] == [tiles(V, n, stats), stats]
+        per = got[2:]
+        join = 1 if splits > 1 else 0
+        assert len(per) == 3 * pieces + join, (route, got)
+        at = 0
+        for p in range(pieces):
+            g, x = per[at], per[at + 1]
+            assert g[1] == grad and x[1] == dx and x[0] == tiles(n, F, dx) * splits, (route, got)
+            at += 2 + (join if p + 1 == pieces else 0)
+            assert per[at][1] == dw, (route, got)
+            at += 1
