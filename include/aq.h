@@ -401,7 +401,8 @@ aq_status aq_usq_create(const aq_usq_desc* desc, const void* codes, const void* 
  * 16 bytes per token and group, and at most 32 MiB of partial sums, allocated
  * with the layer): serialise such calls on one stream.
  * X and Y must not overlap.  The layer's device has to be the current one
- * (AQ_ERR_INVALID_ARGUMENT).
+ * (AQ_ERR_INVALID_ARGUMENT).  AQ_ERR_UNSUPPORTED: n times the larger feature
+ * count past some 2^36 in one call.
  */
 aq_status aq_usq_forward(aq_usq* layer, const void* X, void* Y, int64_t n, void* stream);
 
@@ -429,8 +430,11 @@ aq_status aq_usq_destroy(aq_usq* layer);
 
 /* ---- losses over a vocabulary ---- */
 
-/* What a low-bit model is tuned with (Sec. 3.2): the losses and their
- * gradients, in the layouts aq_layer_codebook_grad and aq_usq_input_grad take. */
+/* What a language model of low-bit layers is tuned with: the losses that its
+ * gradients start from, and their gradients, in the layouts that
+ * aq_layer_codebook_grad and aq_usq_input_grad take.  (The AQUATIC-Diff paper
+ * tunes a diffusion model, by the squared difference of predicted means, which
+ * is not here.) */
 typedef struct aq_loss aq_loss; /* opaque, owned by the library */
 
 typedef struct {
@@ -480,10 +484,13 @@ aq_status aq_loss_create(const aq_loss_desc* desc, aq_loss** out);
  * The first call with dX or with dW allocates its workspace (synchronous;
  * refused with AQ_ERR_UNSUPPORTED on a stream under graph capture): 2 bytes
  * per token and vocabulary row of a piece (at most 128 MiB, or 256 rows; twice
- * that for both gradients in fp16), for dX fp32 sums (4 bytes per token and feature unless one piece holds the
- * vocabulary, or up to 64 MiB), for dW a copy of X.  Later calls are
- * asynchronous and allocate nothing.  Calls on one handle share its workspace:
- * serialise them on one stream.  Summation orders are fixed: repeated calls
+ * that for both gradients in fp16), for dX fp32 sums (4 bytes per token and
+ * feature unless one piece holds the vocabulary, or up to 64 MiB), for dW a
+ * copy of X.  A piece holds what max_tokens leave of it, whatever n is.  Later
+ * calls are asynchronous and allocate nothing.  AQ_ERR_UNSUPPORTED: n times the
+ * vocabulary or the features past some 2^36 in one call.  Calls on one handle
+ * share its workspace: serialise them on one stream.  Summation orders are
+ * fixed: repeated calls
  * give identical bits.
  */
 aq_status aq_loss_cross_entropy(aq_loss* loss_handle, const void* X, const void* W, const int64_t* targets,

@@ -20,8 +20,8 @@
 //    tile's columns, and the transposing LDS read gathers a lane's eight values
 //    of K from eight rows, four at a time.  Row r's slots are moved by 4 (r & 3),
 //    so that the four rows of a read lie in different bank groups.
-//  * Measured, 256 x 256 tiles, bf16: 16384 x 4096 x 4096 0.40 ms, 1.37 PFLOP/s,
-//    where a library's 8192^3 reaches 1.36; transposed operands 0.40 to 0.44 ms.
+//  * Measured, 256 x 256 tiles, bf16: 16384 x 4096 x 4096 0.41 ms, 1.33 PFLOP/s,
+//    where a library's 8192^3 reaches 1.36; transposed operands 0.42 to 0.46 ms.
 //    The matrix cores bound it, at the clock that the power leaves them.
 //  * Rows past M or N are read from the last row (their results are dropped);
 //    slots past K are read from a block of zeros.

@@ -377,8 +377,8 @@ struct RowState {          // arrays of n tokens each
 
 // D rows are vocabulary rows, D columns tokens: a lane's values all belong to
 // one token, so a tile's maximum and sum are reductions over registers.  4096 x
-// 4096 x 131072 bf16: 3.27 ms, 1.34 PFLOP/s, bound by the products; 2048 x 1024
-// x 50021: 0.21 ms, 1.0 (16 chunks a tile, an exponential for every 1024 of K).
+// 4096 x 131072 bf16: 3.38 ms, 1.30 PFLOP/s, bound by the products; 2048 x 1024
+// x 50021: 0.24 ms, 0.88 (16 chunks a tile, an exponential for every 1024 of K).
 template <int WM, int WN, int AM, int AN>
 struct StatsEpilogue {
     float2* part;          // [tiles_m][n]
@@ -456,7 +456,7 @@ __device__ __forceinline__ float row_weight(const RowState& rs, int64_t t) {
 // written (zeros past the ends): the products that read them walk whole 16-byte
 // groups.  Neighbouring lanes hold neighbouring tokens: each pair of lanes swaps
 // half of its values, so that every store carries two tokens of a row.  4096 x
-// 4096 x 131072 bf16: 3.57 ms, 1.23 PFLOP/s, products, exponentials and stores.
+// 4096 x 131072 bf16: 3.67 ms, 1.20 PFLOP/s, products, exponentials and stores.
 enum GradScale {
     GRAD_CALL = 1,         // scaled by the call's peak
     GRAD_OWN = 2,          // by each token's own

@@ -406,21 +406,26 @@ __global__ void __launch_bounds__(256) usq_sums_kernel(UsqArgs a, int group) {
     }
 }
 
-// A 2 x 2 grid of waves on a (64 AM) x (64 AN) tile of tokens x output rows;
-// wave tiles of 32 AM x 32 AN in blocks of v_mfma_f32_32x32x16 (D rows: tokens,
+// WM x WN waves (four) on a tile of 32 WM AM tokens x 32 WN AN output rows, each
+// on 32 AM x 32 AN of it in blocks of v_mfma_f32_32x32x16 (D rows: tokens,
 // columns: output rows, so that a lane has one scale a block and group).
+// Launched as 1 x 4 waves on 128 x 128: every wave all of the tile's tokens, so
+// that no two waves widen the same codes.
 //  * The tile's tokens reach LDS 128 inputs at a time through direct-to-LDS
 //    loads, in two stages (slots permuted as in gemm_mainloop, sixteen a row).
 //  * Weights go from the code tiles to registers, are widened there once a
 //    chunk, and serve all of the wave's tokens; no LDS traffic.
-//  * A group's sum accumulates on its own (two token blocks at a time, four
-//    independent chains) and is scaled into the running sum.
+//  * A group's sum accumulates on its own (AM x AN independent chains) and is
+//    scaled into the running sum.
 //  * The zero points come first: -s z times the group sums is a product over
 //    groups, of s z in two bf16 pieces (15 bits at most, exact) and the sums in
 //    three, six of the eight values a lane holds for one group.
-// Bound by issue slots and the clock under load: besides 32 matrix instructions
-// a chunk takes a wave 56 instructions that widen and 64 that scale.  4096 x
-// 4096 -> 4096 bf16, group 128: some 138 us of a 146 us call, 1.0 PFLOP/s.
+// A chunk takes a wave 32 matrix instructions (1024 cycles of its SIMD's matrix
+// core) and some 200 vector ones (800 cycles; 56 widen, 64 scale, the rest are
+// moves, addresses and the tile's ends).  4096 x 4096 -> 4096 bf16, group 128:
+// 154 us, 0.89 PFLOP/s; counters at 2.0 GHz: the matrix cores are busy for 48 %
+// of the time, the vector ALUs for 36 %, and the two waves of a SIMD hardly
+// overlap one with the other.
 // SG: steps of 16 inputs a group within a chunk.
 template <int DT, int SG, int WM, int WN, int AM, int AN>
 __global__ void __launch_bounds__(256, 2) usq_gemm_kernel(UsqArgs a) {
