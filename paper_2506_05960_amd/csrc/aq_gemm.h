@@ -447,28 +447,29 @@ hipError_t launch_store_gemm(const GemmOperands& g, const GemmPlan& p, const Sto
 }
 
 // out[m][n] = unscaled (sum over the splits, in split order), four values a thread (N a multiple of 8).
-template <int DT>
+// OWN: by the rows' own peaks.
+template <int DT, bool OWN>
 __global__ void __launch_bounds__(256) split_sum_kernel(const float* sum, int splits, int64_t M, int N, uint16_t* out,
                                                         int64_t ldo, const float* peak, const float* own) {
-    const float call = peak ? grad_unscale(*peak) : 1.0f;
+    const float call = !OWN && peak ? grad_unscale(*peak) : 1.0f;
     const int64_t count = M * N;
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)gridDim.x * 1024) {
         floatx4 v = *reinterpret_cast<const floatx4*>(sum + i);
 #pragma unroll 8
         for (int z = 1; z < splits; ++z) v += *reinterpret_cast<const floatx4*>(sum + z * count + i);
         const int64_t m = i / N;
-        const float f = own ? grad_unscale(own[m]) : call;
+        const float f = OWN ? grad_unscale(own[m]) : call;
         *reinterpret_cast<uint2*>(out + m * ldo + (i - m * N)) =
             make_uint2(f32_to_tile<DT>(v[0] * f) | (uint32_t)f32_to_tile<DT>(v[1] * f) << 16,
                        f32_to_tile<DT>(v[2] * f) | (uint32_t)f32_to_tile<DT>(v[3] * f) << 16);
     }
 }
 
-template <int DT>
+template <int DT, bool OWN>
 hipError_t launch_split_sum(const float* sum, int splits, int64_t M, int N, uint16_t* out, int64_t ldo,
                             const float* peak, const float* own, hipStream_t st) {
     const int64_t blocks = (M * N + 1023) / 1024;
-    split_sum_kernel<DT><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, peak, own);
+    split_sum_kernel<DT, OWN><<<(unsigned)std::min<int64_t>(blocks, 8192), 256, 0, st>>>(sum, splits, M, N, out, ldo, peak, own);
     return hipGetLastError();
 }
 

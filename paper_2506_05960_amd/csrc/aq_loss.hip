@@ -682,7 +682,7 @@ static hipError_t cross_entropy(aq_loss* L, const uint16_t* X, const uint16_t* W
                       : (first ? launch_store_gemm<DT, true, STORE_SUM>(d, px, s, st)
                                : launch_store_gemm<DT, true, STORE_ADD>(d, px, s, st));
             if (e == hipSuccess && last && !whole)
-                e = launch_split_sum<DT>(L->d_dx, px.splits, n, F, dX, F, rs.peak, own, st);
+                e = launch_split_sum<DT, own_peaks(DT)>(L->d_dx, px.splits, n, F, dX, F, rs.peak, own, st);
             if (e != hipSuccess) return e;
         }
         if (dW) {

@@ -913,7 +913,7 @@ hipError_t launch_few_grad(const UsqArgs& a, const uint16_t* dy, int cp, float* 
     else if (a.n <= 32) usq_few_grad_kernel<DT, SG, 2><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
     else usq_few_grad_kernel<DT, SG, 4><<<grid, 256, 0, st>>>(a, dy, cp, rows, sum);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_split_sum<DT>(sum, splits, a.n, a.K, dX, a.K, nullptr, nullptr, st);
+    return e != hipSuccess ? e : launch_split_sum<DT, false>(sum, splits, a.n, a.K, dX, a.K, nullptr, nullptr, st);
 }
 
 // dst[r][c] of pitch cp = src[r][c], zero for C <= c < cp.
@@ -960,7 +960,7 @@ hipError_t input_grad(const aq_usq* L, const UsqArgs& a, const uint16_t* dY, uin
                          : launch_store_gemm<DT, false, STORE_OUT>(g, p, s, st);
         if (e != hipSuccess) return e;
         if (p.splits > 1 &&
-            (e = launch_split_sum<DT>(L->d_dsum, p.splits, n, cols, dX + k0, K, nullptr, nullptr, st)) != hipSuccess)
+            (e = launch_split_sum<DT, false>(L->d_dsum, p.splits, n, cols, dX + k0, K, nullptr, nullptr, st)) != hipSuccess)
             return e;
     }
     return hipSuccess;
