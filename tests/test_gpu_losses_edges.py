@@ -75,3 +75,54 @@ def test_cross_entropy_rows_of_far_smaller_weights(dtype, n, V, both):
     ddz = weight * (dz.abs() * (eps / 2) + 2 * (p + (dz - p).abs()) * rel + peak * 2.0 ** -39)
     want, b = (weight * dz) @ w, ddz @ w + (V + 64) * TL.U * ((weight * dz).abs() @ w)
     assert TL.within(dx, want, b + TL.half_step(want.abs() + b, dtype))
+
+
+def test_distill_offsets_past_32_bits():
+    """2.2 thousand million logits: 64 rows over and over, so that every block of 64 has to repeat the first."""
+    V, n, top = 131073, 64 * 263, 5
+    assert n * V > 1 << 31
+    g = torch.Generator().manual_seed(3)
+    z = torch.randn(64, V, generator=g).to(torch.bfloat16)
+    ids = torch.randint(0, V, (64, top), generator=g).int()
+    ids[:, 0] = V - 1
+    t = torch.randn(64, top, generator=g).to(torch.bfloat16)
+    many = z.cuda().repeat(n // 64, 1)
+    loss, grad = TL.losses(V, n=n).distill(many, ids.cuda().repeat(n // 64, 1), t.cuda().repeat(n // 64, 1), 1.5, grad=many)
+    rows = torch.tensor([0, 31, 63])
+    TL.check_distill(z[rows], ids[rows], t[rows], 1.5, torch.ones(3), "bf16", loss[rows], grad[rows])
+    assert torch.equal(loss, loss[:64].repeat(n // 64))
+    for at in range(64, n, 64 * 37):
+        assert torch.equal(grad[at:at + 64], grad[:64])
+    assert torch.equal(grad[-64:], grad[:64])
+
+
+def test_cross_entropy_offsets_past_32_bits():
+    """A head of 4.5 GB: 1000 rows over and over, the targets in the last ones.  Bounds as in test_gpu_losses.py."""
+    n, F, unique, times = 5, 4096, 1000, 550
+    V = unique * times
+    assert V * F * 2 > 1 << 32
+    x, w, _, dloss = TL.ce_inputs(n, F, unique, "bf16", 12)
+    targets = torch.tensor([V - 1, V - 1000, 0, V - 500, -1], device="cuda")
+    loss, dx, dw = TL.losses(V, F, "bf16", n).cross_entropy(x, w.repeat(times, 1), targets, dloss, dx=True, dw=True)
+    z, counts = x.double() @ w.double().t(), targets >= 0
+    log_p = torch.log_softmax(z, dim=1) - math.log(times)
+    at = targets.clamp(min=0) % unique
+    rows = torch.arange(n, device="cuda")
+    most = z.abs().amax(dim=1)
+    rel = TL.U * (2 * 1.4427 * most + 4 + V / 256 + 300)
+    assert TL.within(loss, -log_p[rows, at] * counts, counts * (2 * rel + 8 * TL.U * (4 * most + math.log2(V) + 8)))
+    # the tokens' own rows of dz, over the unique rows (for dX their sum over the repeats) and at the targets
+    weight = (dloss.double() * counts)[:, None]
+    p = log_p.exp()
+    one = torch.zeros_like(p)
+    one[rows, at] = 1
+    half = torch.finfo(torch.bfloat16).eps / 2
+    want = (weight * (p * times - one)) @ w.double()
+    size = (weight * (p * times + one)) @ w.double().abs()
+    assert TL.within(dx, want, size * (half + 2 * float(rel.max()) + (V + 64) * TL.U) + TL.half_step(want, "bf16"))
+    for first in (0, unique * (times // 2), V - unique):
+        here = one * ((targets >= first) & (targets < first + unique))[:, None]
+        want = (weight * (p - here)).t() @ x.double()
+        size = (weight * (p + here)).t() @ x.double().abs()
+        got = dw[first:first + unique]
+        assert TL.within(got, want, size * (half + 2 * float(rel.max()) + 128 * TL.U) + TL.half_step(want.abs() + size * half, "bf16"))

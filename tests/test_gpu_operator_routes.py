@@ -119,3 +119,24 @@ def test_distill(n, vocab, dtype):
     assert torch.equal(L.distill(zg, ig, tg, 1.5, dloss=dg)[0], loss)
     again, _ = L.distill(zg, ig, tg, 1.5, dloss=dg, grad=zg)
     assert torch.equal(again, loss) and torch.equal(zg, grad)
+
+
+def test_many_tokens_offsets_past_32_bits():
+    """Outputs of 2.2 thousand million values: 128 tokens over and over, so that every block repeats the first."""
+    n, wide = 128 * 1100, 16000
+    assert n * wide > 1 << 31
+    for K, C_out, call in ((8, wide, "forward"), (wide, 8, "input_grad")):
+        codes, scales, z, W, mag = TU.make(K, C_out, 128, "bf16", True, seed=9)
+        lay = TU.layer_of(codes, scales, z, 128, "bf16", "bf16", n)
+        x = torch.randn(128, 8, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+        got = getattr(lay, call)(x.repeat(n // 128, 1))
+        W64 = W.t().cuda() if call == "forward" else W.cuda()
+        want = x.double() @ W64
+        bound = 24 * TU.U32 * (x.double().abs() @ (mag.t().cuda() if call == "forward" else W64.abs()))
+        if call == "input_grad":
+            bound = bound + x.double().abs() @ TU.half_step(W64, "bf16")
+        assert bool(((got[:128].double() - want).abs() <= bound + TU.half_step(want.abs() + bound, "bf16")).all())
+        for at in [*range(128, n, 128 * 97), n - 128]:
+            assert torch.equal(got[at:at + 128], got[:128])
+        lay.close()
+        del got
